@@ -184,7 +184,9 @@ def prepare(case, seed):
         from paper_2402_11809_amd import binding
         model = _head_model(case["vocab"])
         pairs = len(_lens(case)) // 2 if case["kind"] == "pref" else 0
-        state.update(model=model, out=binding.LossOut(model, state["rows"], grad_dtype=state["logits"].dtype, pairs=pairs))
+        # dlogits of sar and policy is the gradient of what is maximised, minus the loss: the calls are asked for it with a factor of -1
+        state.update(model=model, out=binding.LossOut(model, state["rows"], grad_dtype=state["logits"].dtype, pairs=pairs),
+                     minus=torch.full((1,), -1.0, device=DEV))
     return state
 
 
@@ -215,11 +217,11 @@ def _run_own(case, s):
         return {"norm": m.grad_clip(s["set"], case["max_norm"]), "grads": s["flat"]}
     out = s["out"]
     if case["kind"] == "sar":
-        m.sar_loss_grad(s["logits"], s["labels"], out, mean=case["mean"])
+        m.sar_loss_grad(s["logits"], s["labels"], out, mean=case["mean"], grad_scale=s["minus"])
         return {"loss": out.loss, "n_terms": out.n_terms, "row_loss": out.row_loss, "dlogits": out.dlogits}
     if case["kind"] == "policy":
         m.policy_loss(s["logits"], s["labels"], s["advantages"], out, old_logp=s["old_logp"], ref_logp=s["ref_logp"], clip_low=CLIP_LOW,
-                      clip_high=CLIP_HIGH, kl_coef=case["kl"], row_weight=s["row_weight"], mean=case["mean"])
+                      clip_high=CLIP_HIGH, kl_coef=case["kl"], row_weight=s["row_weight"], mean=case["mean"], grad_scale=s["minus"])
         return {"loss": out.loss, "n_terms": out.n_terms, "row_loss": out.row_loss, "row_logp": out.row_logp, "n_clipped": out.n_clipped,
                 "dlogits": out.dlogits}
     m.preference_loss(s["logits"], s["labels"], s["seq_start"], out, ref_logp=s["ref_logp"], beta=BETA, margin=MARGIN, smoothing=case["smoothing"],
