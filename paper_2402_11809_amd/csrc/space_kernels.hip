@@ -3474,14 +3474,6 @@ hipError_t launch_sample_verify(const SampleLaunch& v, hipStream_t s) {
 // float4 loads.
 constexpr int kNllThreads = 512, kNllHeld = 32;  // logits of a row a thread takes at a time
 
-// e^d for d <= 0 within about an ulp: p = d log2(e) is rounded to 32 bits, which alone would put up to 1e-6 on an
-// exponential of -20 and a bias on the sums; what it lost, d - p ln 2, goes back in behind the hardware's exponential (0.9 us
-// of the 37 above).  d = -inf (a masked logit) gives 0: the difference is no number there, and the maximum drops it; NaN stays NaN.
-__device__ __forceinline__ float exp_below(float d) {
-    const float p = d * 1.4426950408889634f, e = __builtin_amdgcn_exp2f(p);
-    return fmaf(e, fmaxf(fmaf(p, -0.6931471805599453f, d), -1.f), e);
-}
-
 template <bool VEC>
 __global__ __launch_bounds__(kNllThreads, 8) void nll_rows_kernel(const float* __restrict__ logits, const int32_t* __restrict__ labels,
                                                                   int vocab, float* __restrict__ row_loss, int32_t* faults) {
