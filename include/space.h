@@ -340,6 +340,105 @@ int space_sar_transform(const int32_t *tokens, int32_t n_prompt, int32_t n_answe
 int space_sar_loss(space_ctx *ctx, const float *logits, const int32_t *labels, int32_t rows, float *row_loss,
                    float *loss_sum, int32_t *n_terms, void *stream);
 
+/* Losses on logits with their gradients.  The logits may come from a step (step_out.logits) or from the caller's
+ * own training forward: only the vocabulary of `ctx` matters.  What the three calls share:
+ *   - row r of the logits predicts labels[r]; a negative label leaves the row out: no term, gradient 0, its logits are not
+ *     looked at.  A label >= vocab is left out too and counted by space_device_faults();
+ *   - logp_r = log softmax(logits[r])[labels[r]].  Logits of -inf are masked tokens (gradient 0).  A row that counts
+ *     and has nothing but -inf, a NaN or a +inf makes its terms and its gradient NaN, as in space_sar_loss;
+ *   - dlogits[r][i] = grad_scale * dL/dlogits[r][i], L being what *loss receives.  It is rounded once, from 32 bits to
+ *     `dtype`.  Sums over rows and what is derived from them are held in 64 bits, exponentials and their sums per thread in 32;
+ *   - every sum has a fixed order: the same inputs give the same bits;
+ *   - all scratch is the caller's (row_logp, row_loss, work), so calls on different streams share nothing.
+ * All pointers are DEVICE.  Elements between vocab and a row's stride are neither read nor written.  dlogits may be
+ * logits itself (same pointer and stride); otherwise the two must not overlap. */
+typedef enum space_dtype { SPACE_F32 = 0, SPACE_BF16 = 1 } space_dtype;
+
+typedef struct space_loss_io {
+    const void *logits;      /* [rows] rows of vocab elements, row r at element r * logits_stride          */
+    const int32_t *labels;   /* [rows]                                                                     */
+    void *dlogits;           /* [rows] rows of vocab elements; NULL: no gradient                           */
+    const float *grad_scale; /* [1] factor of the gradient (loss scaling, accumulation); NULL: 1           */
+    float *loss;             /* [1]                                                                        */
+    int32_t *n_terms;        /* [1]     rows that count                                                    */
+    float *row_logp;         /* [rows]  logp of every row that counts, 0 elsewhere                         */
+    float *row_loss;         /* [rows]  the rows' terms, 0 where they do not count (not used by space_preference_loss) */
+    void *work;              /* [rows * SPACE_LOSS_WORK] bytes of scratch, on 16 bytes                     */
+    int64_t logits_stride;   /* elements, >= vocab */
+    int64_t dlogits_stride;
+    int32_t rows;
+    int32_t dtype;           /* space_dtype of logits and dlogits */
+    int32_t mean;            /* 0: L is the sum of the terms; 1: divided by their number (of rows or, in
+                                space_preference_loss, of pairs; by 1 where there are none) */
+} space_loss_io;
+#define SPACE_LOSS_WORK 16 /* bytes a row */
+
+/* The loss of space_sar_loss with its gradient: term_r = -logp_r.  Asynchronous on `stream`, no allocation.
+ * Errors of all three: SPACE_EINVAL (null pointer, rows < 1, stride below vocab, unknown dtype, dlogits overlapping logits,
+ * a parameter out of its range). */
+int space_sar_loss_grad(space_ctx *ctx, const space_loss_io *io, void *stream);
+
+/* Clipped policy loss with a KL term, for rollouts of this model (labels = the tokens that were generated):
+ *   q = exp(logp - old_logp), u = q * advantage, c = clamp(q, 1 - clip_low, 1 + clip_high) * advantage,
+ *   term = row_weight * (-min(u, c) + kl_coef * (exp(d) - d - 1)),  d = ref_logp - logp.
+ * The gradient of a row whose u is above its c (clipped) is that of the KL term alone; at u == c it is u's. */
+typedef struct space_policy_params {
+    const float *advantages; /* [rows] */
+    const float *old_logp;   /* [rows] logp under the model that generated the tokens; NULL: logp itself, held constant (q = 1) */
+    const float *ref_logp;   /* [rows] logp under the reference model; needed where kl_coef != 0, otherwise may be NULL */
+    const float *row_weight; /* [rows]; NULL: 1 */
+    float *row_kl;           /* [rows] exp(d) - d - 1 of every row that counts, or NULL; 0 without ref_logp */
+    int32_t *n_clipped;      /* [1]    rows that are clipped, or NULL */
+    float clip_low;          /* 0 .. 1 */
+    float clip_high;         /* >= 0   */
+    float kl_coef;           /* >= 0   */
+} space_policy_params;
+int space_policy_loss(space_ctx *ctx, const space_loss_io *io, const space_policy_params *params, void *stream);
+
+/* Preference loss of paired log ratios.  Sequence s is the rows seq_start[s] .. seq_start[s+1] - 1; the sequences of a
+ * pair stand side by side, the chosen one (2p) in front of the rejected one (2p + 1).  S_s is the sum of logp over the rows
+ * of s that count (average: their mean; 0 for a sequence without any).
+ *   z = beta * ((S_2p - ref_2p) - (S_2p+1 - ref_2p+1)) - margin
+ *   term_p = (1 - smoothing) * softplus(-z) + smoothing * softplus(z)
+ * Rows in front of the first and behind the last sequence do not count.  Offsets outside 0 .. rows or in falling order are
+ * clamped and counted by space_device_faults(). */
+typedef struct space_preference_params {
+    const int32_t *seq_start; /* [2 * pairs + 1] */
+    const float *ref_logp;    /* [2 * pairs] S under the reference model (a mean where average is set); NULL: 0 */
+    float *pair_loss;         /* [pairs]     the terms */
+    float *seq_logp;          /* [2 * pairs] S, or NULL */
+    int32_t pairs;
+    int32_t average;
+    float beta;               /* > 0 */
+    float margin;
+    float smoothing;          /* 0 .. 1 */
+} space_preference_params;
+int space_preference_loss(space_ctx *ctx, const space_loss_io *io, const space_preference_params *params, void *stream);
+
+/* The 2-norm over all gradients of a model, and clipping to it.  `tensors` is a HOST array, read before the call returns
+ * (nothing of it is kept); its pointers are DEVICE.  Any number of tensors, of mixed types, of any length
+ * (0 included) and any alignment of whole elements. */
+typedef struct space_grad_tensor {
+    const void *grad;
+    void *out;         /* where space_grad_clip writes; may be grad itself (same dtype) */
+    int64_t n;         /* elements, contiguous */
+    int32_t dtype;     /* space_dtype */
+    int32_t out_dtype;
+} space_grad_tensor;
+#define SPACE_GRAD_WORK 2048 /* doubles of scratch */
+
+/* *norm = sqrt(sum of squares), squares and sums in 64 bits (no overflow in between) and in an order that depends on the
+ * tensors' lengths and types alone.  n_tensors == 0 gives 0.  `out` is not looked at.
+ *   norm  DEVICE float32 [1];   work  DEVICE float64 [SPACE_GRAD_WORK], overwritten
+ * Errors: SPACE_EINVAL (null, negative length, unknown dtype, pointer that is not on a whole element). */
+int space_grad_norm(space_ctx *ctx, const space_grad_tensor *tensors, int32_t n_tensors, float *norm, double *work, void *stream);
+
+/* out = grad * max_norm / *norm where *norm is above max_norm and finite, else out = grad (a norm that is not finite
+ * leaves the gradients as they are: the caller finds it in *norm and skips the step).
+ *   norm  DEVICE float32 [1], of space_grad_norm or of the caller (several processes that added up their squares)
+ * Errors: as space_grad_norm; max_norm negative or NaN; an `out` that overlaps anything but its own equal grad. */
+int space_grad_clip(space_ctx *ctx, const space_grad_tensor *tensors, int32_t n_tensors, const float *norm, float max_norm, void *stream);
+
 /* Tuning hook (not part of the method).  space_init reads the environment variable SPACE_TUNE once, a
  * comma-separated list of overrides of what it would otherwise pick by itself:
  *   qkv=R:S, o=R:S, gu=R:S, dn=R:S, lm=R:S   tiling of one projection: R weight tiles per wave (2, 4, 6, 8)

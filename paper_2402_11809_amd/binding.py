@@ -22,7 +22,8 @@ STATUS_NAMES = {0: "SPACE_OK", -1: "SPACE_EINVAL", -2: "SPACE_ESHAPE", -3: "SPAC
 
 EXPORTS = ["space_last_error", "space_init", "space_load_layer", "space_destroy", "space_layout_create", "space_layout_destroy",
            "space_kv_bytes", "space_kv_reset", "space_step", "space_kv_commit", "space_kv_rollback",
-           "space_sample_verify", "space_sample_verify_static", "space_sar_loss", "space_sar_transform", "space_prefill", "space_kv_pool_bytes", "space_device_faults", "space_debug_buffer", "space_timing_enable",
+           "space_sample_verify", "space_sample_verify_static", "space_sar_loss", "space_sar_loss_grad", "space_policy_loss", "space_preference_loss", "space_grad_norm",
+           "space_grad_clip", "space_sar_transform", "space_prefill", "space_kv_pool_bytes", "space_device_faults", "space_debug_buffer", "space_timing_enable",
            "space_timing_read", "space_tune_rows"]
 
 KERNEL_CLASSES = ["embed", "norm", "qkv", "rope", "attn", "o", "gate_up", "down", "lm_head", "verify"]
@@ -76,6 +77,33 @@ class SpaceSampleIO(C.Structure):
                 ("finished", C.c_void_p)]
 
 
+class SpaceLossIO(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("labels", C.c_void_p), ("dlogits", C.c_void_p), ("grad_scale", C.c_void_p),
+                ("loss", C.c_void_p), ("n_terms", C.c_void_p), ("row_logp", C.c_void_p), ("row_loss", C.c_void_p),
+                ("work", C.c_void_p), ("logits_stride", C.c_int64), ("dlogits_stride", C.c_int64), ("rows", C.c_int32),
+                ("dtype", C.c_int32), ("mean", C.c_int32)]
+
+
+class SpacePolicyParams(C.Structure):
+    _fields_ = [("advantages", C.c_void_p), ("old_logp", C.c_void_p), ("ref_logp", C.c_void_p), ("row_weight", C.c_void_p),
+                ("row_kl", C.c_void_p), ("n_clipped", C.c_void_p), ("clip_low", C.c_float), ("clip_high", C.c_float),
+                ("kl_coef", C.c_float)]
+
+
+class SpacePreferenceParams(C.Structure):
+    _fields_ = [("seq_start", C.c_void_p), ("ref_logp", C.c_void_p), ("pair_loss", C.c_void_p), ("seq_logp", C.c_void_p),
+                ("pairs", C.c_int32), ("average", C.c_int32), ("beta", C.c_float), ("margin", C.c_float), ("smoothing", C.c_float)]
+
+
+class SpaceGradTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32), ("out_dtype", C.c_int32)]
+
+
+SPACE_F32, SPACE_BF16 = 0, 1
+SPACE_LOSS_WORK = 16    # bytes of scratch a row of logits
+SPACE_GRAD_WORK = 2048  # doubles
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -123,6 +151,14 @@ def load_library():
     lib.space_tune_rows.argtypes = [vp, i32, vp]
     lib.space_sar_loss.restype = C.c_int
     lib.space_sar_loss.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp]
+    for name, params in (("space_sar_loss_grad", ()), ("space_policy_loss", (C.POINTER(SpacePolicyParams),)),
+                         ("space_preference_loss", (C.POINTER(SpacePreferenceParams),))):
+        getattr(lib, name).restype = C.c_int
+        getattr(lib, name).argtypes = [vp, C.POINTER(SpaceLossIO), *params, vp]
+    lib.space_grad_norm.restype = C.c_int
+    lib.space_grad_norm.argtypes = [vp, C.POINTER(SpaceGradTensor), i32, vp, vp, vp]
+    lib.space_grad_clip.restype = C.c_int
+    lib.space_grad_clip.argtypes = [vp, C.POINTER(SpaceGradTensor), i32, vp, C.c_float, vp]
     i32p = C.POINTER(C.c_int32)
     lib.space_sar_transform.restype = C.c_int
     lib.space_sar_transform.argtypes = [i32p, i32, i32, i32, i32, C.c_float, C.c_float, C.c_float, i32p, i32p, i32p, i32p, i32p]
@@ -285,6 +321,86 @@ class SampleOut:
         self.ratios = torch.empty(batch, max(n_groups - 1, 1), dtype=f32, device=dev)
 
 
+def _dtype_code(dtype) -> int:
+    import torch
+    assert dtype in (torch.float32, torch.bfloat16), f"float32 or bfloat16, not {dtype}"
+    return SPACE_F32 if dtype == torch.float32 else SPACE_BF16
+
+
+class LossOut:
+    """Device buffers for the outputs and the scratch of sar_loss_grad, policy_loss and preference_loss, allocated once and
+    reused: `rows` rows of logits, `pairs` pairs (preference_loss).  grad_dtype: the logits' type, for a gradient `dlogits`
+    [rows, vocab] of its own; or dlogits: a tensor of the caller's with unit column stride (the logits themselves, too);
+    neither: no gradient.  Two calls that may overlap in time need a LossOut each."""
+
+    def __init__(self, model: "Model", rows: int, grad_dtype=None, dlogits=None, pairs: int = 0):
+        import torch
+        dev, i32, f32 = model.device, torch.int32, torch.float32
+        rows, pairs = int(rows), int(pairs)
+        assert rows >= 1 and pairs >= 0
+        if dlogits is None and grad_dtype is not None:
+            _dtype_code(grad_dtype)
+            dlogits = torch.empty(rows, model.cfg.vocab, dtype=grad_dtype, device=dev)
+        if dlogits is not None:
+            _dtype_code(dlogits.dtype)
+            assert dlogits.device == dev and dlogits.dim() == 2 and dlogits.shape == (rows, model.cfg.vocab)
+            assert dlogits.stride(1) == 1 or model.cfg.vocab == 1, "dlogits needs unit column stride"
+        self.rows, self.pairs, self.dlogits = rows, pairs, dlogits
+        self.loss = torch.zeros(1, dtype=f32, device=dev)
+        self.n_terms = torch.zeros(1, dtype=i32, device=dev)
+        self.row_logp = torch.zeros(rows, dtype=f32, device=dev)
+        self.row_loss = torch.zeros(rows, dtype=f32, device=dev)
+        self.row_kl = torch.zeros(rows, dtype=f32, device=dev)
+        self.n_clipped = torch.zeros(1, dtype=i32, device=dev)
+        self.pair_loss = torch.zeros(pairs, dtype=f32, device=dev) if pairs else None
+        self.seq_logp = torch.zeros(2 * pairs, dtype=f32, device=dev) if pairs else None
+        self.work = torch.empty(rows * SPACE_LOSS_WORK // 4, dtype=f32, device=dev)
+        self.c = SpaceLossIO(None, None, _ptr(dlogits), None, _ptr(self.loss), _ptr(self.n_terms), _ptr(self.row_logp),
+                             _ptr(self.row_loss), _ptr(self.work), 0, _row_stride(dlogits), rows,
+                             -1 if dlogits is None else _dtype_code(dlogits.dtype), 0)
+
+
+def _row_stride(t) -> int:
+    """Elements from one row to the next (torch gives a lone row any stride)."""
+    return 0 if t is None else max(int(t.stride(0)), int(t.shape[1])) if t.shape[0] == 1 else int(t.stride(0))
+
+
+class GradSet:
+    """The gradients of a model as space_grad_norm / space_grad_clip take them: `grads` CUDA tensors (float32 or bfloat16, dense in
+    any order of dimensions), `outs` where the clipped ones go (same shapes and strides; None: in place).  Reusable as long as the
+    tensors stay where they are, which the set sees to by holding them; norm and scratch belong to the set."""
+
+    def __init__(self, model: "Model", grads: Sequence[object], outs: Optional[Sequence[object]] = None):
+        import torch
+        self.model, self.grads = model, list(grads)
+        self.outs = self.grads if outs is None else list(outs)
+        assert len(self.outs) == len(self.grads)
+        self.c = (SpaceGradTensor * max(len(self.grads), 1))()
+        for i, (g, o) in enumerate(zip(self.grads, self.outs)):
+            for t in (g, o):
+                assert t.device == model.device and _dense(t), f"tensor {i}: not a dense tensor on {model.device}"
+            assert g.shape == o.shape and (g is o or _same_order(g, o)), f"tensor {i}: gradient and output laid out differently"
+            self.c[i] = SpaceGradTensor(_ptr(g), _ptr(o), g.numel(), _dtype_code(g.dtype), _dtype_code(o.dtype))
+        self.norm = torch.zeros(1, dtype=torch.float32, device=model.device)
+        self.work = torch.empty(SPACE_GRAD_WORK, dtype=torch.float64, device=model.device)
+
+
+def _dense(t) -> bool:
+    """Whether the elements fill one run of memory, in whatever order of dimensions."""
+    want = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
+        if size == 0:
+            return True
+        if stride != want:
+            return False
+        want *= size
+    return True
+
+
+def _same_order(a, b) -> bool:
+    return all(x == y for x, y, n in zip(a.stride(), b.stride(), a.shape) if n > 1) or a.numel() == 0
+
+
 class Model:
     """space_ctx of one model.  `weights` maps tensor names to CUDA bf16 tensors:
     embed [V+1, d], final_norm [d], lm_head [V, d], layers: list of dicts with attn_norm wq wk wv wo
@@ -415,6 +531,77 @@ class Model:
         self._check(self.lib.space_sar_loss(self.ctx, _ptr(logits), _ptr(labels), rows, _ptr(row_loss), _ptr(loss), _ptr(n),
                                             _stream(stream)))
         return loss, n
+
+    def _loss_io(self, logits, labels, out: LossOut, grad_scale, mean: bool) -> SpaceLossIO:
+        import torch
+        assert logits.device == self.device and labels.device == self.device and torch.cuda.current_device() == self.device.index
+        assert logits.dim() == 2 and logits.shape == (out.rows, self.cfg.vocab) and (logits.stride(1) == 1 or self.cfg.vocab == 1)
+        assert labels.dtype is torch.int32 and labels.shape == (out.rows,) and labels.is_contiguous()
+        if grad_scale is not None:
+            assert grad_scale.dtype is torch.float32 and grad_scale.device == self.device and grad_scale.numel() == 1
+        io = out.c
+        code = _dtype_code(logits.dtype)
+        assert out.dlogits is None or out.dlogits.dtype == logits.dtype, "dlogits has the type of the logits"
+        io.logits, io.labels, io.grad_scale = logits.data_ptr(), labels.data_ptr(), _ptr(grad_scale)
+        io.logits_stride, io.dtype, io.mean = _row_stride(logits), code, int(bool(mean))
+        return io
+
+    def _rows_arg(self, t, n: int, name: str) -> Optional[int]:
+        import torch
+        if t is None:
+            return None
+        assert t.dtype is torch.float32 and t.device == self.device and t.is_contiguous() and t.numel() == n, name
+        return t.data_ptr()
+
+    def sar_loss_grad(self, logits, labels, out: LossOut, mean: bool = False, grad_scale=None, stream=None) -> None:
+        """space_sar_loss_grad: logits [rows, vocab] float32 or bfloat16 with unit column stride, labels int32 [rows], CUDA.
+        Fills out.loss, n_terms, row_loss, row_logp and, if `out` has one, dlogits."""
+        io = self._loss_io(logits, labels, out, grad_scale, mean)
+        self._check(self.lib.space_sar_loss_grad(self.ctx, C.byref(io), _stream(stream)))
+
+    def policy_loss(self, logits, labels, advantages, out: LossOut, old_logp=None, ref_logp=None, clip_low: float = 0.2,
+                    clip_high: float = 0.2, kl_coef: float = 0.0, row_weight=None, mean: bool = True, grad_scale=None,
+                    stream=None) -> None:
+        """space_policy_loss: advantages, old_logp, ref_logp and row_weight are float32 [rows].  Fills out.loss, n_terms,
+        row_loss, row_logp, row_kl, n_clipped and, if `out` has one, dlogits."""
+        io = self._loss_io(logits, labels, out, grad_scale, mean)
+        assert advantages is not None
+        rows = out.rows
+        p = SpacePolicyParams(self._rows_arg(advantages, rows, "advantages"), self._rows_arg(old_logp, rows, "old_logp"),
+                              self._rows_arg(ref_logp, rows, "ref_logp"), self._rows_arg(row_weight, rows, "row_weight"),
+                              _ptr(out.row_kl), _ptr(out.n_clipped), float(clip_low), float(clip_high), float(kl_coef))
+        self._check(self.lib.space_policy_loss(self.ctx, C.byref(io), C.byref(p), _stream(stream)))
+
+    def preference_loss(self, logits, labels, seq_start, out: LossOut, ref_logp=None, beta: float = 0.1, margin: float = 0.0,
+                        smoothing: float = 0.0, average: bool = False, mean: bool = True, grad_scale=None, stream=None) -> None:
+        """space_preference_loss: seq_start int32 [2 * out.pairs + 1], ref_logp float32 [2 * out.pairs].  Fills out.loss, n_terms,
+        pair_loss, seq_logp, row_logp and, if `out` has one, dlogits."""
+        import torch
+        io = self._loss_io(logits, labels, out, grad_scale, mean)
+        assert out.pairs >= 1 and seq_start.dtype is torch.int32 and seq_start.device == self.device
+        assert seq_start.is_contiguous() and seq_start.numel() == 2 * out.pairs + 1
+        p = SpacePreferenceParams(seq_start.data_ptr(), self._rows_arg(ref_logp, 2 * out.pairs, "ref_logp"), _ptr(out.pair_loss),
+                                  _ptr(out.seq_logp), out.pairs, int(bool(average)), float(beta), float(margin), float(smoothing))
+        self._check(self.lib.space_preference_loss(self.ctx, C.byref(io), C.byref(p), _stream(stream)))
+
+    def grad_norm(self, grads: GradSet, stream=None):
+        """space_grad_norm: the 2-norm over the set, as the one-element CUDA tensor grads.norm."""
+        import torch
+        assert grads.model is self and torch.cuda.current_device() == self.device.index
+        self._check(self.lib.space_grad_norm(self.ctx, grads.c, len(grads.grads), grads.norm.data_ptr(), grads.work.data_ptr(),
+                                             _stream(stream)))
+        return grads.norm
+
+    def grad_clip(self, grads: GradSet, max_norm: float, norm=None, stream=None):
+        """space_grad_norm (unless `norm`, a float32 one-element CUDA tensor, is given) and space_grad_clip: the clipped gradients
+        go to grads.outs.  Returns the norm."""
+        import torch
+        if norm is None:
+            norm = self.grad_norm(grads, stream)
+        assert grads.model is self and torch.cuda.current_device() == self.device.index
+        assert norm.dtype is torch.float32 and norm.numel() == 1 and norm.device == self.device
+        self._check(self.lib.space_grad_clip(self.ctx, grads.c, len(grads.grads), norm.data_ptr(), float(max_norm), _stream(stream)))
+        return norm
 
     def kv_commit(self, kv: KVCache, accepted_len=None, accepted_all: int = 0, stream=None) -> None:
         rc = self.lib.space_kv_commit(self.ctx, C.byref(kv.c), _ptr(accepted_len), int(accepted_all), _stream(stream))

@@ -11,11 +11,13 @@
 #include <mutex>
 #include <new>
 #include <map>
+#include <memory>
 #include <string>
 #include <vector>
 
 #include "../../include/space.h"
 #include "space_kernels.h"
+#include "space_train_plan.h"
 
 using namespace space;
 
@@ -552,6 +554,67 @@ int run_gemm(space_ctx* ctx, const PackedW& w, GemmEpilogue epi, const uint16_t*
     if (splits_used) *splits_used = w.splits;
     if (groups_used) *groups_used = gemm_groups(w, g.tiles_per_wave);
     HIP_TRY(ctx, launch_gemm(g, epi, s));
+    return SPACE_OK;
+}
+
+}  // namespace
+
+namespace {
+
+size_t dtype_bytes(int dtype) { return dtype == SPACE_F32 ? 4 : dtype == SPACE_BF16 ? 2 : 0; }
+
+// The checks that the losses share, and their common arguments as the kernels take them.
+int loss_launch(space_ctx* ctx, const char* who, const space_loss_io* io, bool row_terms, LossLaunch* l) {
+    if (!io || !io->logits || !io->labels || !io->loss || !io->n_terms || !io->row_logp || !io->work || (row_terms && !io->row_loss))
+        return fail(ctx, SPACE_EINVAL, "%s: null argument", who);
+    const int vocab = ctx->cfg.vocab;
+    const size_t b = dtype_bytes(io->dtype);
+    if (!b) return fail(ctx, SPACE_EINVAL, "%s: unknown dtype %d", who, io->dtype);
+    if (io->rows < 1 || io->logits_stride < vocab || (io->dlogits && io->dlogits_stride < vocab))
+        return fail(ctx, SPACE_EINVAL, "%s: no rows, or a row stride below the vocabulary of %d", who, vocab);
+    const int64_t most = INT64_MAX / 16 / io->rows;
+    if (io->logits_stride > most || (io->dlogits && io->dlogits_stride > most)) return fail(ctx, SPACE_EINVAL, "%s: row stride out of range", who);
+    const uintptr_t x = (uintptr_t)io->logits, d = (uintptr_t)io->dlogits;
+    if (x % b || d % b || (uintptr_t)io->work % 16)
+        return fail(ctx, SPACE_EINVAL, "%s: logits or dlogits not on a whole element, or work not on 16 bytes", who);
+    if (io->dlogits && !(x == d && io->logits_stride == io->dlogits_stride)) {
+        if (!rows_apart(x, io->logits_stride, d, io->dlogits_stride, io->rows, vocab, b))
+            return fail(ctx, SPACE_EINVAL, "%s: dlogits overlaps logits", who);
+    }
+    *l = LossLaunch{};
+    l->logits = io->logits; l->labels = io->labels; l->dlogits = io->dlogits; l->grad_scale = io->grad_scale;
+    l->loss = io->loss; l->n_terms = io->n_terms; l->row_logp = io->row_logp; l->row_loss = io->row_loss;
+    l->work = (f32x4_raw*)io->work;
+    l->logits_stride = io->logits_stride; l->dlogits_stride = io->dlogits_stride;
+    l->rows = io->rows; l->vocab = vocab; l->dtype = io->dtype; l->mean = io->mean != 0;
+    l->faults = ctx->faults;
+    return SPACE_OK;
+}
+
+// Checks a list of gradients and copies it.  writes: `out` is written, so no range that is written may meet another one (but
+// for a gradient that is clipped in place): their order would decide the result.
+int grad_list(space_ctx* ctx, const char* who, const space_grad_tensor* t, int32_t n, bool writes, std::unique_ptr<GradTensor[]>* list) {
+    if (n < 0 || (n > 0 && !t)) return fail(ctx, SPACE_EINVAL, "%s: null or negative list", who);
+    std::unique_ptr<ByteRange[]> ranges;
+    list->reset(new (std::nothrow) GradTensor[n > 0 ? n : 1]);
+    if (writes) ranges.reset(new (std::nothrow) ByteRange[2 * (size_t)n + 1]);
+    if (!*list || (writes && !ranges)) return fail(ctx, SPACE_ENOMEM, "%s: no host memory for a list of %d", who, n);
+    size_t m = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        const size_t gb = dtype_bytes(t[i].dtype), ob = dtype_bytes(t[i].out_dtype);
+        if (!gb || (writes && !ob)) return fail(ctx, SPACE_EINVAL, "%s: tensor %d: unknown dtype", who, i);
+        if (t[i].n < 0 || t[i].n > INT64_MAX / 8) return fail(ctx, SPACE_EINVAL, "%s: tensor %d: length %lld", who, i, (long long)t[i].n);
+        (*list)[i] = GradTensor{t[i].grad, writes ? t[i].out : nullptr, t[i].n, t[i].dtype, writes ? t[i].out_dtype : t[i].dtype};
+        if (t[i].n == 0) continue;
+        const uintptr_t g = (uintptr_t)t[i].grad, o = (uintptr_t)t[i].out;
+        if (!g || (writes && !o)) return fail(ctx, SPACE_EINVAL, "%s: tensor %d: null pointer", who, i);
+        if (g % gb || (writes && o % ob)) return fail(ctx, SPACE_EINVAL, "%s: tensor %d: not on a whole element", who, i);
+        if (!writes) continue;
+        if (!(g == o && gb == ob)) ranges[m++] = ByteRange{g, g + (uintptr_t)t[i].n * gb, false};
+        ranges[m++] = ByteRange{o, o + (uintptr_t)t[i].n * ob, true};
+    }
+    if (writes && !written_apart(ranges.get(), m))
+        return fail(ctx, SPACE_EINVAL, "%s: an output overlaps another tensor of the list", who);
     return SPACE_OK;
 }
 
@@ -1128,6 +1191,71 @@ int space_sar_transform(const int32_t* tokens, int32_t n_prompt, int32_t n_answe
     *n_labels = n_prompt + m + k;  // the original tokens through y_{m+k}
     for (int i = 0; i < *n_labels; ++i) labels[i] = tokens[i];
     *m_out = m;
+    return SPACE_OK;
+}
+
+int space_sar_loss_grad(space_ctx* ctx, const space_loss_io* io, void* stream) {
+    if (!ctx) return SPACE_EINVAL;
+    LossLaunch l;
+    if (int rc = loss_launch(ctx, "space_sar_loss_grad", io, true, &l)) return rc;
+    HIP_TRY(ctx, launch_sar_grad(l, (hipStream_t)stream));
+    return SPACE_OK;
+}
+
+int space_policy_loss(space_ctx* ctx, const space_loss_io* io, const space_policy_params* params, void* stream) {
+    if (!ctx) return SPACE_EINVAL;
+    const char* who = "space_policy_loss";
+    LossLaunch l;
+    if (int rc = loss_launch(ctx, who, io, true, &l)) return rc;
+    if (!params || !params->advantages) return fail(ctx, SPACE_EINVAL, "%s: null argument", who);
+    if (!(params->clip_low >= 0.f && params->clip_low <= 1.f) || !(params->clip_high >= 0.f) || !std::isfinite(params->clip_high) ||
+        !(params->kl_coef >= 0.f) || !std::isfinite(params->kl_coef))
+        return fail(ctx, SPACE_EINVAL, "%s: clip_low %g outside 0..1, or clip_high %g or kl_coef %g negative or not finite", who,
+                    (double)params->clip_low, (double)params->clip_high, (double)params->kl_coef);
+    if (params->kl_coef != 0.f && !params->ref_logp) return fail(ctx, SPACE_EINVAL, "%s: kl_coef needs ref_logp", who);
+    PolicyArgs p{};
+    p.advantages = params->advantages; p.old_logp = params->old_logp; p.ref_logp = params->ref_logp;
+    p.row_weight = params->row_weight; p.row_kl = params->row_kl; p.n_clipped = params->n_clipped;
+    p.lo = 1.f - params->clip_low; p.hi = 1.f + params->clip_high; p.kl_coef = params->kl_coef;
+    HIP_TRY(ctx, launch_policy(l, p, (hipStream_t)stream));
+    return SPACE_OK;
+}
+
+int space_preference_loss(space_ctx* ctx, const space_loss_io* io, const space_preference_params* params, void* stream) {
+    if (!ctx) return SPACE_EINVAL;
+    const char* who = "space_preference_loss";
+    LossLaunch l;
+    if (int rc = loss_launch(ctx, who, io, false, &l)) return rc;
+    if (!params || !params->seq_start || !params->pair_loss) return fail(ctx, SPACE_EINVAL, "%s: null argument", who);
+    if (params->pairs < 1 || params->pairs > INT32_MAX / 2 - 1) return fail(ctx, SPACE_EINVAL, "%s: %d pairs", who, params->pairs);
+    if (!(params->beta > 0.f) || !std::isfinite(params->beta) || !std::isfinite(params->margin) || !(params->smoothing >= 0.f && params->smoothing <= 1.f))
+        return fail(ctx, SPACE_EINVAL, "%s: beta %g not above 0, margin %g not finite or smoothing %g outside 0..1", who,
+                    (double)params->beta, (double)params->margin, (double)params->smoothing);
+    PrefArgs p{};
+    p.seq_start = params->seq_start; p.ref_logp = params->ref_logp; p.pair_loss = params->pair_loss; p.seq_logp = params->seq_logp;
+    p.pairs = params->pairs; p.average = params->average != 0;
+    p.beta = params->beta; p.margin = params->margin; p.smoothing = params->smoothing;
+    HIP_TRY(ctx, launch_preference(l, p, (hipStream_t)stream));
+    return SPACE_OK;
+}
+
+int space_grad_norm(space_ctx* ctx, const space_grad_tensor* tensors, int32_t n_tensors, float* norm, double* work, void* stream) {
+    if (!ctx) return SPACE_EINVAL;
+    static_assert(SPACE_GRAD_WORK == kGradParts, "the header states the size of the scratch");
+    if (!norm || !work) return fail(ctx, SPACE_EINVAL, "space_grad_norm: null argument");
+    std::unique_ptr<GradTensor[]> list;
+    if (int rc = grad_list(ctx, "space_grad_norm", tensors, n_tensors, false, &list)) return rc;
+    HIP_TRY(ctx, launch_grad_norm(list.get(), n_tensors, norm, work, (hipStream_t)stream));
+    return SPACE_OK;
+}
+
+int space_grad_clip(space_ctx* ctx, const space_grad_tensor* tensors, int32_t n_tensors, const float* norm, float max_norm, void* stream) {
+    if (!ctx) return SPACE_EINVAL;
+    if (!norm) return fail(ctx, SPACE_EINVAL, "space_grad_clip: null argument");
+    if (!(max_norm >= 0.f)) return fail(ctx, SPACE_EINVAL, "space_grad_clip: max_norm %g negative or not a number", (double)max_norm);
+    std::unique_ptr<GradTensor[]> list;
+    if (int rc = grad_list(ctx, "space_grad_clip", tensors, n_tensors, true, &list)) return rc;
+    HIP_TRY(ctx, launch_grad_clip(list.get(), n_tensors, norm, max_norm, (hipStream_t)stream));
     return SPACE_OK;
 }
 

@@ -16,6 +16,8 @@ constexpr int kMaxRowTiles = 6;   // 96 rows per projection pass; also the longe
 constexpr int kMaxBlockRows = 1024;  // longest block of one sequence (prompt chunks; no verification beyond 96 rows)
 constexpr int kAttnKeys = 32;     // keys per attention chunk; V is stored transposed in runs of 32
 
+struct __attribute__((aligned(16))) f32x4_raw { float v[4]; };
+
 enum GemmEpilogue { EPI_F32 = 0, EPI_SWIGLU = 1, EPI_ARGMAX = 2 };
 
 // Shape of an activation matrix X[rows, k] in operand ("tile") order.  Contraction tile kt holds,
@@ -355,6 +357,50 @@ hipError_t launch_sample_verify(const SampleLaunch& v, hipStream_t s);
 // order and n_terms = the number of rows that count.
 hipError_t launch_nll(const float* logits, const int32_t* labels, int rows, int vocab, float* row_loss, float* loss_sum,
                       int32_t* n_terms, int32_t* faults, hipStream_t s);
+
+// Losses on logits with their gradients (space_train.hip).  Strides in elements; dlogits NULL: no gradient.
+enum LossKind { LOSS_SAR = 0, LOSS_POLICY = 1, LOSS_PREF = 2 };
+struct LossLaunch {
+    const void* logits;
+    const int32_t* labels;
+    void* dlogits;
+    const float* grad_scale;
+    float* loss;
+    int32_t* n_terms;
+    float* row_logp;
+    float* row_loss;
+    f32x4_raw* work;  // [rows], see the kernels
+    int64_t logits_stride, dlogits_stride;
+    int rows, vocab, dtype, mean;
+    int32_t* faults;
+};
+struct PolicyArgs {
+    const float *advantages, *old_logp, *ref_logp, *row_weight;
+    float* row_kl;
+    int32_t* n_clipped;
+    float lo, hi, kl_coef;  // bounds of the clamp
+};
+struct PrefArgs {
+    const int32_t* seq_start;
+    const float* ref_logp;
+    float *pair_loss, *seq_logp;
+    int pairs, average;
+    float beta, margin, smoothing;
+};
+hipError_t launch_sar_grad(const LossLaunch& l, hipStream_t s);
+hipError_t launch_policy(const LossLaunch& l, const PolicyArgs& p, hipStream_t s);
+hipError_t launch_preference(const LossLaunch& l, const PrefArgs& p, hipStream_t s);
+
+// Gradient norm and clipping.  work: [kGradParts] partial sums of squares.
+constexpr int kGradParts = 2048;
+struct GradTensor {
+    const void* grad;
+    void* out;
+    int64_t n;
+    int dtype, out_dtype;
+};
+hipError_t launch_grad_norm(const GradTensor* t, int n, float* norm, double* work, hipStream_t s);
+hipError_t launch_grad_clip(const GradTensor* t, int n, const float* norm, float max_norm, hipStream_t s);
 
 hipError_t launch_kv_len_update(int32_t* len, int batch, const int32_t* delta_dev, int delta_all, int sign,
                                 int clamp_hi, int capacity, hipStream_t s);
