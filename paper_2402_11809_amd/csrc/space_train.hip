@@ -17,19 +17,36 @@ template <typename T> __device__ __forceinline__ void store_f32(T* p, float v);
 template <> __device__ __forceinline__ void store_f32<float>(float* p, float v) { *p = v; }
 template <> __device__ __forceinline__ void store_f32<uint16_t>(uint16_t* p, float v) { *p = f2bf(v); }
 
-constexpr int kRowThreads = 256;
+// 16 bytes of a row, on any whole element (the hardware takes them unaligned)
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+    static constexpr int N = 4;
+    typedef float raw __attribute__((ext_vector_type(4), aligned(4)));
+    static __device__ __forceinline__ void get(raw q, float* v) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = q[e];
+    }
+    static __device__ __forceinline__ raw put(const float* v) { return raw{v[0], v[1], v[2], v[3]}; }
+};
+template <> struct Vec<uint16_t> {
+    static constexpr int N = 8;
+    typedef uint32_t raw __attribute__((ext_vector_type(4), aligned(2)));
+    static __device__ __forceinline__ void get(raw q, float* v) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t w = q[e];
+            v[2 * e] = __uint_as_float(w << 16);
+            v[2 * e + 1] = __uint_as_float(w & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ raw put(const float* v) {
+        raw q;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[e] = (uint32_t)f2bf(v[2 * e]) | (uint32_t)f2bf(v[2 * e + 1]) << 16;
+        return q;
+    }
+};
 
-template <int W>
-__device__ __forceinline__ float block_max(float v, float* s) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < W; ++w) v = fmaxf(v, s[w]);
-    return v;
-}
 template <int W>
 __device__ __forceinline__ double block_sum(double v, double* s) {
 #pragma unroll
@@ -43,102 +60,316 @@ __device__ __forceinline__ double block_sum(double v, double* s) {
     return v;
 }
 
-struct RowFacts {
-    float top;      // m
-    double others;  // O
-    double total;   // T
-    double logp;
-};
-
-template <typename T>
-__device__ __forceinline__ RowFacts row_facts(const T* __restrict__ x, int vocab, int label) {
-    constexpr int W = kRowThreads / 64;
-    __shared__ float s_max[W];
-    __shared__ double s_sum[W];
-    float mx = -INFINITY;
-    for (int i = threadIdx.x; i < vocab; i += kRowThreads) mx = fmaxf(mx, load_f32(x + i));
-    RowFacts f;
-    f.top = block_max<W>(mx, s_max);
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < vocab; i += kRowThreads)
-        if (i != label) sum += exp_below(load_f32(x + i) - f.top);
-    f.others = block_sum<W>(sum, s_sum);
-    const float d = load_f32(x + label) - f.top;
-    f.total = f.others + exp_below(d);
-    f.logp = (double)d - (d == 0.f ? log1p(f.others) : log(f.total));
-    return f;
-}
-
-// d logits of one row: slope = c above, times the caller's scale
-template <typename T>
-__device__ __forceinline__ void row_gradient(const T* x, T* __restrict__ d, int vocab, int label, float top, float per_e, float at_label) {
-    for (int i = threadIdx.x; i < vocab; i += kRowThreads)
-        store_f32(d + i, i == label ? at_label : per_e * exp_below(load_f32(x + i) - top));
-}
-template <typename T>
-__device__ __forceinline__ void row_zero(T* __restrict__ d, int vocab) {
-    for (int i = threadIdx.x; i < vocab; i += kRowThreads) store_f32(d + i, 0.f);
-}
-
 // Whether row `label` counts; one that lies behind the vocabulary is a fault of the caller's.
 __device__ __forceinline__ bool row_counts(int label, int vocab) { return label >= 0 && label < vocab; }
 
-template <typename T, int KIND>
-__global__ __launch_bounds__(kRowThreads) void loss_rows_kernel(LossLaunch l, PolicyArgs p) {
-    const int row = blockIdx.x, label = l.labels[row];
-    const T* x = (const T*)l.logits + (size_t)row * l.logits_stride;
-    T* d = l.dlogits ? (T*)l.dlogits + (size_t)row * l.dlogits_stride : nullptr;
-    if (!row_counts(label, l.vocab)) {
-        if (threadIdx.x == 0) {
-            l.row_logp[row] = 0.f;
-            if (KIND != LOSS_PREF) l.row_loss[row] = 0.f;
-            if (KIND == LOSS_POLICY && p.row_kl) p.row_kl[row] = 0.f;
-            l.work[row] = f32x4_raw{{0.f, 0.f, 0.f, 0.f}};
-            if (label >= 0) atomicAdd(l.faults, 1);
-        }
-        if (KIND != LOSS_PREF && d) row_zero(d, l.vocab);
-        return;
+template <typename T, int THREADS>
+__device__ __forceinline__ void row_zero(T* __restrict__ d, int vocab) {
+    typedef Vec<T> V;
+    const float none[V::N] = {};
+    for (int i = threadIdx.x * V::N; i < vocab / V::N * V::N; i += THREADS * V::N) __builtin_nontemporal_store(V::put(none), (typename V::raw*)(d + i));
+    if ((int)threadIdx.x < vocab % V::N) store_f32(d + vocab / V::N * V::N + threadIdx.x, 0.f);
+}
+
+// What a row's label and its other tokens add up to, in the row's own scale (its maximum)
+struct RowFacts {
+    float top;
+    float at_label;  // e_y
+    double others;   // O
+    double total;    // T
+    __device__ __forceinline__ double logp(float x_label) const {
+        const float d = x_label - top;
+        return (double)d - (d == 0.f ? log1p(others) : log(total));
     }
-    const RowFacts f = row_facts(x, l.vocab, label);
-    if (KIND == LOSS_PREF) {
-        if (threadIdx.x == 0) {
-            l.row_logp[row] = (float)f.logp;
-            l.work[row] = f32x4_raw{{f.top, (float)(1.0 / f.total), (float)(f.others / f.total), 0.f}};
-        }
-        return;
+};
+
+// Joins the waves' maxima and sums (without the label's): one barrier a row.  *factor: from the wave's scale to the row's.
+template <int W>
+__device__ __forceinline__ RowFacts join_waves(float mx, double sum, float x_label, float* factor, float* s_max, double* s_sum) {
+    if ((threadIdx.x & 63) == 0) {
+        s_max[threadIdx.x >> 6] = mx;
+        s_sum[threadIdx.x >> 6] = sum;
     }
-    double slope = -1.0, term = -f.logp, clipped = 0.0;
+    __syncthreads();
+    RowFacts f;
+    f.top = x_label;
+#pragma unroll
+    for (int w = 0; w < W; ++w) f.top = fmaxf(f.top, s_max[w]);
+    f.others = 0.0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) f.others += s_sum[w] * (s_max[w] == -INFINITY ? 0.f : exp_below(s_max[w] - f.top));
+    f.at_label = exp_below(x_label - f.top);
+    f.total = f.others + f.at_label;
+    *factor = mx == -INFINITY ? 0.f : exp_below(mx - f.top);
+    return f;
+}
+
+struct RowSlope {
+    double term, slope, kl;
+    bool clipped;
+};
+template <int KIND>
+__device__ __forceinline__ RowSlope row_slope(const PolicyArgs& p, int row, double logp) {
+    RowSlope s{-logp, -1.0, 0.0, false};
     if (KIND == LOSS_POLICY) {
-        const double a = p.advantages[row], q = p.old_logp ? exp(f.logp - p.old_logp[row]) : 1.0;
+        const double a = p.advantages[row], q = p.old_logp ? exp(logp - p.old_logp[row]) : 1.0;
         const double u = q * a, c = fmin(fmax(q, (double)p.lo), (double)p.hi) * a;
-        clipped = u > c ? 1.0 : 0.0;
-        term = u > c ? -c : -u;
-        slope = u > c ? 0.0 : -u;
-        double kl = 0.0;
+        s.clipped = u > c;
+        s.term = s.clipped ? -c : -u;
+        s.slope = s.clipped ? 0.0 : -u;
         if (p.ref_logp) {
-            const double gap = p.ref_logp[row] - f.logp, em = expm1(gap);
-            kl = em - gap;
+            const double gap = p.ref_logp[row] - logp, em = expm1(gap);
+            s.kl = em - gap;
             if (p.kl_coef != 0.f) {
-                term += (double)p.kl_coef * kl;
-                slope -= (double)p.kl_coef * em;
+                s.term += (double)p.kl_coef * s.kl;
+                s.slope -= (double)p.kl_coef * em;
             }
         }
         if (p.row_weight) {
-            term *= p.row_weight[row];
-            slope *= p.row_weight[row];
+            s.term *= p.row_weight[row];
+            s.slope *= p.row_weight[row];
         }
-        if (threadIdx.x == 0 && p.row_kl) p.row_kl[row] = (float)kl;
     }
+    return s;
+}
+
+// What a row that does not count leaves behind.
+template <typename T, int KIND, int THREADS>
+__device__ __forceinline__ void row_left_out(const LossLaunch& l, const PolicyArgs& p, int row, int label, T* d) {
     if (threadIdx.x == 0) {
-        l.row_logp[row] = (float)f.logp;
-        l.row_loss[row] = (float)term;
-        l.work[row] = f32x4_raw{{(float)clipped, 0.f, 0.f, 0.f}};
+        l.row_logp[row] = 0.f;
+        if (KIND != LOSS_PREF) l.row_loss[row] = 0.f;
+        if (KIND == LOSS_POLICY && p.row_kl) p.row_kl[row] = 0.f;
+        l.work[row] = f32x4_raw{{0.f, 0.f, 0.f, 0.f}};
+        if (label >= 0) atomicAdd(l.faults, 1);
     }
-    if (!d) return;
-    double c = slope;
-    if (l.mean) c /= max(*l.n_terms, 1);
+    if (KIND != LOSS_PREF && d) row_zero<T, THREADS>(d, l.vocab);
+}
+
+// The row's own outputs, by thread 0.  Returns the slope of the loss along logp.
+template <int KIND>
+__device__ __forceinline__ double row_outputs(const LossLaunch& l, const PolicyArgs& p, int row, const RowFacts& f, float x_label) {
+    const double logp = f.logp(x_label);
+    l.row_logp[row] = (float)logp;
+    if (KIND == LOSS_PREF) {
+        l.work[row] = f32x4_raw{{f.top, (float)(1.0 / f.total), (float)(f.others / f.total), 0.f}};
+        return 0.0;
+    }
+    const RowSlope s = row_slope<KIND>(p, row, logp);
+    l.row_loss[row] = (float)s.term;
+    if (KIND == LOSS_POLICY) {
+        l.work[row] = f32x4_raw{{s.clipped ? 1.f : 0.f, 0.f, 0.f, 0.f}};
+        if (p.row_kl) p.row_kl[row] = (float)s.kl;
+    }
+    return s.slope;
+}
+// What the gradient of the loss along logp is multiplied with.
+__device__ __forceinline__ double slope_factor(const LossLaunch& l) {
+    double c = l.mean ? 1.0 / max(*l.n_terms, 1) : 1.0;
     if (l.grad_scale) c *= *l.grad_scale;
-    row_gradient(x, d, l.vocab, label, f.top, (float)(-c / f.total), (float)(c * (f.others / f.total)));
+    return c;
+}
+// The slope with everything in it, for all threads; the policy loss has it from thread 0.
+template <int KIND>
+__device__ __forceinline__ float row_coefficient(const LossLaunch& l, const PolicyArgs& p, int row, const RowFacts& f, float x_label, float* s_slope) {
+    if (KIND == LOSS_SAR) return (float)-slope_factor(l);
+    if (threadIdx.x == 0) *s_slope = (float)(row_outputs<KIND>(l, p, row, f, x_label) * slope_factor(l));
+    __syncthreads();
+    return *s_slope;
+}
+
+// A row in the registers of one workgroup: read once, written once.  Bound by memory: a row that is read while another one
+// of the CU is computed or written, so what counts is that two rows or more share a CU (128 registers a thread, four waves a
+// SIMD).  32 elements a thread in short rows, 64 in longer ones.  KEEP: the exponentials take the logits' place, 32 bits each;
+// otherwise (bf16 rows that would fill the CU that way) the packed logits stay and the exponential is taken again.
+// 5.77 TB/s read and written in fp32 (4096 rows of 32000, 182 us), 5.46 in bf16 (8192 rows, 192 us), where a copy of such
+// buffers reaches 4.8 - 4.9; all in one launch of 1024 threads and 32 elements 5.0 and 4.0.  Loads and stores are non-temporal:
+// stores 5.1 -> 5.5 TB/s.
+template <typename T, int KIND, int THREADS, int NV, bool KEEP>
+__global__ __launch_bounds__(THREADS, 4) void loss_rows_kernel(LossLaunch l, PolicyArgs p) {
+    typedef Vec<T> V;
+    constexpr int W = THREADS / 64, E = V::N;
+    __shared__ float s_max[W], s_slope;
+    __shared__ double s_sum[W];
+    const int row = blockIdx.x, tid = threadIdx.x, label = l.labels[row], vocab = l.vocab;
+    const T* x = (const T*)l.logits + (size_t)row * l.logits_stride;
+    T* d = l.dlogits ? (T*)l.dlogits + (size_t)row * l.dlogits_stride : nullptr;
+    if (!row_counts(label, vocab)) return row_left_out<T, KIND, THREADS>(l, p, row, label, d);
+    const float x_label = load_f32(x + label);
+    // whole vectors, then the odd elements behind them, one to a thread
+    const int whole = vocab / E, odd = whole * E + tid;
+    typename V::raw q[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (tid + j * THREADS < whole) q[j] = __builtin_nontemporal_load((const typename V::raw*)(x + (size_t)(tid + j * THREADS) * E));
+    float t = odd < vocab && odd != label ? load_f32(x + odd) : -INFINITY;
+    float v[KEEP ? NV * E : E], mx = t;
+    // vector j as 32-bit numbers, nothing behind the row and nothing at the label, which stands apart
+    auto unpack = [&](int j, float* u) {
+        if (tid + j * THREADS < whole) {
+            V::get(q[j], u);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) u[e] = -INFINITY;
+        }
+        if (tid + j * THREADS == label / E) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e == label % E) u[e] = -INFINITY;
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (j * THREADS < whole) {  // (all threads or none)
+            float* u = v + (KEEP ? j * E : 0);
+            unpack(j, u);
+#pragma unroll
+            for (int e = 0; e < E; ++e) mx = fmaxf(mx, u[e]);
+        }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+    const float base = mx == -INFINITY ? 0.f : mx;
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (j * THREADS < whole) {
+            float* u = v + (KEEP ? j * E : 0);
+            if (!KEEP) unpack(j, u);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                u[e] = exp_below(u[e] - base);
+                part[e % 4] += u[e];
+            }
+        }
+    }
+    t = exp_below(t - base);
+    double sum = ((double)part[0] + part[1]) + ((double)part[2] + part[3]) + t;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    float factor;
+    const RowFacts f = join_waves<W>(mx, sum, x_label, &factor, s_max, s_sum);
+    if (KIND == LOSS_PREF || !d) {
+        if (tid == 0) row_outputs<KIND>(l, p, row, f, x_label);
+        return;
+    }
+    const float c = row_coefficient<KIND>(l, p, row, f, x_label, &s_slope);
+    const float inv = 1.f / (float)f.total, per_e = -c * inv * factor, at_label = c * ((float)f.others / (float)f.total);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (tid + j * THREADS < whole) {
+            float g[E];
+            float* u = v + (KEEP ? j * E : 0);
+            if (!KEEP) {
+                V::get(q[j], u);
+#pragma unroll
+                for (int e = 0; e < E; ++e) u[e] = __builtin_amdgcn_exp2f((u[e] - base) * 1.4426950408889634f);
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) g[e] = u[e] * per_e;
+            if (tid + j * THREADS == label / E) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (e == label % E) g[e] = at_label;
+            }
+            __builtin_nontemporal_store(V::put(g), (typename V::raw*)(d + (size_t)(tid + j * THREADS) * E));
+        }
+    if (odd < vocab) store_f32(d + odd, odd == label ? at_label : t * per_e);
+    if (KIND == LOSS_SAR && tid == 0) row_outputs<KIND>(l, p, row, f, x_label);
+}
+
+// A row that no workgroup's registers hold: once for maximum and sum, once for the gradient.
+constexpr int kLongThreads = 1024, kLongVecs = 4;
+template <typename T>
+__device__ __forceinline__ void long_gradient(const T* x, T* d, int vocab, int label, float top, float per_e, float at_label) {
+    typedef Vec<T> V;
+    constexpr int E = V::N;
+    const int whole = vocab / E, odd = whole * E + threadIdx.x;
+    for (int at = threadIdx.x; at < whole; at += kLongThreads * kLongVecs) {
+        typename V::raw q[kLongVecs];
+#pragma unroll
+        for (int j = 0; j < kLongVecs; ++j)
+            if (at + j * kLongThreads < whole) q[j] = *(const typename V::raw*)(x + (size_t)(at + j * kLongThreads) * E);
+#pragma unroll
+        for (int j = 0; j < kLongVecs; ++j) {
+            const int i = at + j * kLongThreads;
+            if (i >= whole) break;
+            float g[E];
+            V::get(q[j], g);
+#pragma unroll
+            for (int e = 0; e < E; ++e) g[e] = per_e * exp_below(g[e] - top);
+            if (i == label / E) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (e == label % E) g[e] = at_label;
+            }
+            __builtin_nontemporal_store(V::put(g), (typename V::raw*)(d + (size_t)i * E));
+        }
+    }
+    if (odd < vocab) store_f32(d + odd, odd == label ? at_label : per_e * exp_below(load_f32(x + odd) - top));
+}
+
+template <typename T, int KIND>
+__global__ __launch_bounds__(kLongThreads) void loss_long_rows_kernel(LossLaunch l, PolicyArgs p) {
+    typedef Vec<T> V;
+    constexpr int W = kLongThreads / 64, E = V::N;
+    __shared__ float s_max[W], s_slope;
+    __shared__ double s_sum[W];
+    const int row = blockIdx.x, tid = threadIdx.x, label = l.labels[row], vocab = l.vocab;
+    const T* x = (const T*)l.logits + (size_t)row * l.logits_stride;
+    T* d = l.dlogits ? (T*)l.dlogits + (size_t)row * l.dlogits_stride : nullptr;
+    if (!row_counts(label, vocab)) return row_left_out<T, KIND, kLongThreads>(l, p, row, label, d);
+    const float x_label = load_f32(x + label);
+    const int whole = vocab / E, odd = whole * E + tid;
+    float mx = odd < vocab && odd != label ? load_f32(x + odd) : -INFINITY;
+    double sum = mx == -INFINITY ? 0.0 : (double)exp_below(mx - mx);
+    for (int at = tid; at < whole; at += kLongThreads * kLongVecs) {
+        float v[kLongVecs * E];
+        float m = mx;
+        typename V::raw q[kLongVecs];
+#pragma unroll
+        for (int j = 0; j < kLongVecs; ++j)
+            if (at + j * kLongThreads < whole) q[j] = *(const typename V::raw*)(x + (size_t)(at + j * kLongThreads) * E);
+#pragma unroll
+        for (int j = 0; j < kLongVecs; ++j) {
+            if (at + j * kLongThreads < whole) {
+                V::get(q[j], v + j * E);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[j * E + e] = -INFINITY;
+            }
+            if (at + j * kLongThreads == label / E) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (e == label % E) v[j * E + e] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) m = fmaxf(m, v[j * E + e]);
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        if (mx != -INFINITY) sum *= exp_below(mx - base);
+        mx = m;
+        float part[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kLongVecs * E; ++i) part[i & 1] += exp_below(v[i] - base);
+        sum += (double)part[0] + part[1];
+    }
+    float top = mx;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    if (mx != -INFINITY) sum *= exp_below(mx - top);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    float factor;
+    const RowFacts f = join_waves<W>(top, sum, x_label, &factor, s_max, s_sum);
+    if (KIND == LOSS_PREF || !d) {
+        if (tid == 0) row_outputs<KIND>(l, p, row, f, x_label);
+        return;
+    }
+    const float c = row_coefficient<KIND>(l, p, row, f, x_label, &s_slope);
+    const float inv = 1.f / (float)f.total;
+    long_gradient(x, d, vocab, label, f.top, -c * inv, c * ((float)f.others / (float)f.total));
+    if (KIND == LOSS_SAR && tid == 0) row_outputs<KIND>(l, p, row, f, x_label);
 }
 
 // How many rows count, for the mean that the rows' gradients need before the rows are done.
@@ -230,19 +461,35 @@ __global__ __launch_bounds__(1024) void pref_pairs_kernel(LossLaunch l, PrefArgs
 }
 
 template <typename T>
-__global__ __launch_bounds__(kRowThreads) void pref_gradient_kernel(LossLaunch l) {
+__global__ __launch_bounds__(kLongThreads) void pref_gradient_kernel(LossLaunch l) {
     const int row = blockIdx.x, label = l.labels[row];
     T* d = (T*)l.dlogits + (size_t)row * l.dlogits_stride;
     const f32x4_raw f = l.work[row];
-    if (!row_counts(label, l.vocab) || f.v[3] == 0.f) return row_zero(d, l.vocab);
-    row_gradient((const T*)l.logits + (size_t)row * l.logits_stride, d, l.vocab, label, f.v[0], -f.v[3] * f.v[1], f.v[3] * f.v[2]);
+    if (!row_counts(label, l.vocab) || f.v[3] == 0.f) return row_zero<T, kLongThreads>(d, l.vocab);
+    long_gradient((const T*)l.logits + (size_t)row * l.logits_stride, d, l.vocab, label, f.v[0], -f.v[3] * f.v[1], f.v[3] * f.v[2]);
 }
 
+template <typename T, int KIND>
+hipError_t launch_rows_of(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) {
+    constexpr int E = Vec<T>::N;
+    const dim3 grid(l.rows);
+#define SPACE_ROWS(THREADS, ELEMS, KEEP) \
+    hipLaunchKernelGGL((loss_rows_kernel<T, KIND, THREADS, ELEMS / E, KEEP>), grid, dim3(THREADS), 0, s, l, p)
+    if (l.vocab <= 64 * 32) SPACE_ROWS(64, 32, true);
+    else if (l.vocab <= 128 * 32) SPACE_ROWS(128, 32, true);
+    else if (l.vocab <= 128 * 64) SPACE_ROWS(128, 64, true);
+    else if (l.vocab <= 256 * 64) SPACE_ROWS(256, 64, true);
+    else if (l.vocab <= 512 * 64) SPACE_ROWS(512, 64, true);
+    else if (sizeof(T) == 4 && l.vocab <= 1024 * 64) SPACE_ROWS(1024, 64, true);
+    else if (sizeof(T) == 2 && l.vocab <= 512 * 128) SPACE_ROWS(512, sizeof(T) == 2 ? 128 : 64, false);
+    else if (sizeof(T) == 2 && l.vocab <= 1024 * 128) SPACE_ROWS(1024, sizeof(T) == 2 ? 128 : 64, false);
+    else hipLaunchKernelGGL((loss_long_rows_kernel<T, KIND>), grid, dim3(kLongThreads), 0, s, l, p);
+#undef SPACE_ROWS
+    return hipGetLastError();
+}
 template <int KIND>
 hipError_t launch_rows(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) {
-    if (l.dtype == 0) hipLaunchKernelGGL((loss_rows_kernel<float, KIND>), dim3(l.rows), dim3(kRowThreads), 0, s, l, p);
-    else hipLaunchKernelGGL((loss_rows_kernel<uint16_t, KIND>), dim3(l.rows), dim3(kRowThreads), 0, s, l, p);
-    return hipGetLastError();
+    return l.dtype == 0 ? launch_rows_of<float, KIND>(l, p, s) : launch_rows_of<uint16_t, KIND>(l, p, s);
 }
 
 template <int KIND>
@@ -264,8 +511,8 @@ hipError_t launch_preference(const LossLaunch& l, const PrefArgs& p, hipStream_t
     hipLaunchKernelGGL(pref_pairs_kernel, dim3(1), dim3(1024), 0, s, l, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !l.dlogits) return e;
-    if (l.dtype == 0) hipLaunchKernelGGL(pref_gradient_kernel<float>, dim3(l.rows), dim3(kRowThreads), 0, s, l);
-    else hipLaunchKernelGGL(pref_gradient_kernel<uint16_t>, dim3(l.rows), dim3(kRowThreads), 0, s, l);
+    if (l.dtype == 0) hipLaunchKernelGGL(pref_gradient_kernel<float>, dim3(l.rows), dim3(kLongThreads), 0, s, l);
+    else hipLaunchKernelGGL(pref_gradient_kernel<uint16_t>, dim3(l.rows), dim3(kLongThreads), 0, s, l);
     return hipGetLastError();
 }
 
