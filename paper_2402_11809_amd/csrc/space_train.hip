@@ -521,7 +521,7 @@ hipError_t launch_preference(const LossLaunch& l, const PrefArgs& p, hipStream_t
 // ------------------------------------------------------------------------------------------
 // A launch takes up to kGradList tensors by value (arguments of a kernel: 4 KB at most), so nothing has to be kept on the device; their elements are cut into
 // chunks that are dealt out to the workgroups in turn.
-constexpr int kGradList = 112, kGradThreads = 256, kGradChunk = 8192;
+constexpr int kGradList = 112, kGradThreads = 256, kGradChunk = kGradThreads * 32;
 struct GradList {
     const void* grad[kGradList];
     void* out[kGradList];
@@ -540,23 +540,62 @@ __device__ __forceinline__ int grad_tensor_of(const GradList& g, int64_t chunk) 
     }
     return lo;
 }
-__device__ __forceinline__ float grad_load(const void* p, int64_t i, bool bf16) {
-    return bf16 ? bf2f(((const uint16_t*)p)[i]) : ((const float*)p)[i];
+
+// What both passes over the gradients read twice comes from the memory-side cache the second time, if it is small enough: the
+// last kGradKept bytes are read in the ordinary way by the norm, and first by the clipping; everything in front of them, which the
+// cache would lose again, is read past it.
+constexpr int64_t kGradKept = 192ll << 20;
+template <bool KEPT, typename V>
+__device__ __forceinline__ typename V::raw read_grad(const void* p) {
+    if (KEPT) return *(const typename V::raw*)p;
+    return __builtin_nontemporal_load((const typename V::raw*)p);
 }
 
-// Squares are exact in 64 bits for both types, and no sum of them leaves the range.
-__global__ __launch_bounds__(kGradThreads) void grad_square_kernel(GradList g, double* work, int first_launch) {
-    __shared__ double s[kGradThreads / 64];
-    double sum = 0.0;
-    const int64_t chunks = g.first[g.count];
-    for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int t = grad_tensor_of(g, c);
-        const int64_t from = (c - g.first[t]) * kGradChunk, to = min(from + kGradChunk, g.n[t]);
-        for (int64_t i = from + threadIdx.x; i < to; i += kGradThreads) {
-            const double v = grad_load(g.grad[t], i, g.type[t] & 1);
-            sum += v * v;
+// The squares of n elements of a chunk, this thread's share.  A square is exact in 64 bits for both types, and no sum of them leaves the range.
+template <typename T, bool KEPT>
+__device__ __forceinline__ double chunk_squares(const T* __restrict__ x, int n) {
+    typedef Vec<T> V;
+    constexpr int E = V::N, NV = kGradChunk / kGradThreads / E;
+    double sum[2] = {0.0, 0.0};
+    const int tid = threadIdx.x;
+    if (n == kGradChunk) {
+        typename V::raw q[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) q[j] = read_grad<KEPT, V>(x + (tid + j * kGradThreads) * E);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float v[E];
+            V::get(q[j], v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e & 1] = fma((double)v[e], (double)v[e], sum[e & 1]);
+        }
+    } else {
+        for (int i = tid; i < n; i += kGradThreads) {
+            const double v = load_f32(x + i);
+            sum[0] = fma(v, v, sum[0]);
         }
     }
+    return sum[0] + sum[1];
+}
+
+// One chunk after another, dealt out to the workgroups; those from kept_from on stay in the cache.
+template <bool KEPT>
+__device__ __forceinline__ double list_squares(const GradList& g, int64_t c, int64_t end) {
+    double sum = 0.0;
+    for (; c < end; c += gridDim.x) {
+        const int t = grad_tensor_of(g, c);
+        const int64_t from = (c - g.first[t]) * kGradChunk;
+        const int n = (int)min((int64_t)kGradChunk, g.n[t] - from);
+        if (g.type[t] & 1) sum += chunk_squares<uint16_t, KEPT>((const uint16_t*)g.grad[t] + from, n);
+        else sum += chunk_squares<float, KEPT>((const float*)g.grad[t] + from, n);
+    }
+    return sum;
+}
+__global__ __launch_bounds__(kGradThreads) void grad_square_kernel(GradList g, int64_t kept_from, double* work, int first_launch) {
+    __shared__ double s[kGradThreads / 64];
+    double sum = list_squares<false>(g, blockIdx.x, kept_from);
+    const int64_t turn = (kept_from + gridDim.x - 1 - blockIdx.x) / gridDim.x;  // how many of those this workgroup had
+    sum += list_squares<true>(g, blockIdx.x + turn * gridDim.x, g.first[g.count]);
     sum = block_sum<kGradThreads / 64>(sum, s);
     if (threadIdx.x == 0) work[blockIdx.x] = first_launch ? sum : work[blockIdx.x] + sum;
 }
@@ -569,29 +608,81 @@ __global__ __launch_bounds__(1024) void grad_norm_kernel(const double* work, int
     if (threadIdx.x == 0) *norm = (float)sqrt(sum);
 }
 
-__global__ __launch_bounds__(kGradThreads) void grad_clip_kernel(GradList g, const float* norm, float max_norm) {
+// N elements as a thread reads or writes them: 16 bytes, or 8 where bf16 goes with fp32, so that neighbouring lanes' stores meet
+template <typename T, int N> struct Some {
+    template <bool KEPT> static __device__ __forceinline__ void load(const T* p, float* v) { Vec<T>::get(read_grad<KEPT, Vec<T>>(p), v); }
+    static __device__ __forceinline__ void store(T* p, const float* v) { __builtin_nontemporal_store(Vec<T>::put(v), (typename Vec<T>::raw*)p); }
+};
+template <> struct Some<uint16_t, 4> {
+    typedef uint32_t raw __attribute__((ext_vector_type(2), aligned(2)));
+    template <bool KEPT> static __device__ __forceinline__ void load(const uint16_t* p, float* v) {
+        const raw q = read_grad<KEPT, Some>(p);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t w = q[e];
+            v[2 * e] = __uint_as_float(w << 16);
+            v[2 * e + 1] = __uint_as_float(w & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ void store(uint16_t* p, const float* v) {
+        raw q;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) q[e] = (uint32_t)f2bf(v[2 * e]) | (uint32_t)f2bf(v[2 * e + 1]) << 16;
+        __builtin_nontemporal_store(q, (raw*)p);
+    }
+};
+// n elements of a chunk, scaled
+template <bool KEPT, typename T, typename O>
+__device__ __forceinline__ void chunk_scale(const T* x, O* y, int n, float scale) {
+    constexpr int E = sizeof(T) == 2 && sizeof(O) == 2 ? 8 : 4, NV = kGradChunk / kGradThreads / E;
+    const int tid = threadIdx.x;
+    if (n == kGradChunk) {
+        float v[NV][E];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) Some<T, E>::template load<KEPT>(x + (tid + j * kGradThreads) * E, v[j]);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[j][e] *= scale;
+            Some<O, E>::store(y + (tid + j * kGradThreads) * E, v[j]);
+        }
+    } else {
+        for (int i = tid; i < n; i += kGradThreads) store_f32(y + i, load_f32(x + i) * scale);
+    }
+}
+
+template <bool KEPT>
+__global__ __launch_bounds__(kGradThreads) void grad_clip_kernel(GradList g, int64_t begin, int64_t end, const float* norm, float max_norm) {
     const float n = *norm;
     const float scale = n > max_norm && n < INFINITY ? max_norm / n : 1.f;
-    const int64_t chunks = g.first[g.count];
-    for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+    for (int64_t c = begin + blockIdx.x; c < end; c += gridDim.x) {
         const int t = grad_tensor_of(g, c);
         if (scale == 1.f && g.out[t] == g.grad[t]) continue;
-        const int64_t from = (c - g.first[t]) * kGradChunk, to = min(from + kGradChunk, g.n[t]);
-        for (int64_t i = from + threadIdx.x; i < to; i += kGradThreads) {
-            const float v = grad_load(g.grad[t], i, g.type[t] & 1) * scale;
-            if (g.type[t] & 2) ((uint16_t*)g.out[t])[i] = f2bf(v); else ((float*)g.out[t])[i] = v;
+        const int64_t from = (c - g.first[t]) * kGradChunk;
+        const int n = (int)min((int64_t)kGradChunk, g.n[t] - from);
+        const void* x = g.grad[t];
+        void* y = g.out[t];
+        switch (g.type[t]) {
+            case 0: chunk_scale<KEPT>((const float*)x + from, (float*)y + from, n, scale); break;
+            case 1: chunk_scale<KEPT>((const uint16_t*)x + from, (float*)y + from, n, scale); break;
+            case 2: chunk_scale<KEPT>((const float*)x + from, (uint16_t*)y + from, n, scale); break;
+            default: chunk_scale<KEPT>((const uint16_t*)x + from, (uint16_t*)y + from, n, scale); break;
         }
     }
 }
 
-// Calls launch(list, workgroups, first) for every kGradList tensors that are not empty.
+int64_t grad_bytes(const GradTensor& t) { return t.n * (t.dtype ? 2 : 4); }
+
+// Calls launch(list, first chunk that is kept) for every kGradList tensors that are not empty.
 template <typename F>
 hipError_t each_grad_list(const GradTensor* t, int n, F launch) {
+    int64_t left = -kGradKept;  // bytes still in front of those that are kept
+    for (int i = 0; i < n; ++i) left += grad_bytes(t[i]);
     GradList g;
-    bool first = true;
     for (int i = 0; i < n;) {
         g.count = 0;
         g.first[0] = 0;
+        int64_t kept_from = 0;
         for (; i < n && g.count < kGradList; ++i) {
             if (t[i].n == 0) continue;
             const int c = g.count++;
@@ -599,25 +690,32 @@ hipError_t each_grad_list(const GradTensor* t, int n, F launch) {
             g.out[c] = t[i].out;
             g.n[c] = t[i].n;
             g.type[c] = (uint8_t)(t[i].dtype | t[i].out_dtype << 1);
-            g.first[c + 1] = g.first[c] + (t[i].n + kGradChunk - 1) / kGradChunk;
+            const int64_t chunks = (t[i].n + kGradChunk - 1) / kGradChunk;
+            g.first[c + 1] = g.first[c] + chunks;
+            if (left > 0) {
+                const int64_t past = (left + kGradChunk * (t[i].dtype ? 2 : 4) - 1) / (kGradChunk * (t[i].dtype ? 2 : 4));
+                kept_from = g.first[c] + (past < chunks ? past : chunks);
+            }
+            left -= grad_bytes(t[i]);
         }
         if (!g.count) break;
-        launch(g, (int)(g.first[g.count] < kGradParts ? g.first[g.count] : kGradParts), first);
+        launch(g, kept_from);
         if (hipError_t e = hipGetLastError()) return e;
-        first = false;
     }
     return hipSuccess;
 }
 
+int grad_workgroups(int64_t chunks) { return (int)(chunks < kGradParts ? chunks : kGradParts); }
+
 hipError_t launch_grad_norm(const GradTensor* t, int n, float* norm, double* work, hipStream_t s) {
+    // a later launch adds to the partial sums of an earlier one, so all of them have as many workgroups
     int parts = 0;
-    // (a later launch adds to the partial sums of an earlier one, so all of them use as many workgroups)
-    int64_t most = 0;
-    const hipError_t count = each_grad_list(t, n, [&](const GradList& g, int wgs, bool) { most = wgs > most ? wgs : most; });
-    if (count != hipSuccess) return count;
-    parts = (int)most;
-    const hipError_t e = each_grad_list(t, n, [&](const GradList& g, int, bool first) {
-        hipLaunchKernelGGL(grad_square_kernel, dim3(parts), dim3(kGradThreads), 0, s, g, work, (int)first);
+    hipError_t e = each_grad_list(t, n, [&](const GradList& g, int64_t) { parts = max(parts, grad_workgroups(g.first[g.count])); });
+    if (e != hipSuccess) return e;
+    int first = 1;
+    e = each_grad_list(t, n, [&](const GradList& g, int64_t kept_from) {
+        hipLaunchKernelGGL(grad_square_kernel, dim3(parts), dim3(kGradThreads), 0, s, g, kept_from, work, first);
+        first = 0;
     });
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, s, work, parts, norm);
@@ -625,8 +723,13 @@ hipError_t launch_grad_norm(const GradTensor* t, int n, float* norm, double* wor
 }
 
 hipError_t launch_grad_clip(const GradTensor* t, int n, const float* norm, float max_norm, hipStream_t s) {
-    return each_grad_list(t, n, [&](const GradList& g, int wgs, bool) {
-        hipLaunchKernelGGL(grad_clip_kernel, dim3(wgs), dim3(kGradThreads), 0, s, g, norm, max_norm);
+    const hipError_t e = each_grad_list(t, n, [&](const GradList& g, int64_t kept_from) {
+        const int64_t end = g.first[g.count];
+        if (kept_from < end) hipLaunchKernelGGL(grad_clip_kernel<true>, dim3(grad_workgroups(end - kept_from)), dim3(kGradThreads), 0, s, g, kept_from, end, norm, max_norm);
+    });
+    if (e != hipSuccess) return e;
+    return each_grad_list(t, n, [&](const GradList& g, int64_t kept_from) {
+        if (kept_from > 0) hipLaunchKernelGGL(grad_clip_kernel<false>, dim3(grad_workgroups(kept_from)), dim3(kGradThreads), 0, s, g, (int64_t)0, kept_from, norm, max_norm);
     });
 }
 
