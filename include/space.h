@@ -349,7 +349,8 @@ int space_sar_loss(space_ctx *ctx, const float *logits, const int32_t *labels, i
  *   - dlogits[r][i] = grad_scale * dL/dlogits[r][i], L being what *loss receives.  It is rounded once, from 32 bits to
  *     `dtype`.  Sums over rows and what is derived from them are held in 64 bits, exponentials and their sums per thread in 32;
  *   - every sum has a fixed order: the same inputs give the same bits;
- *   - all scratch is the caller's (row_logp, row_loss, work), so calls on different streams share nothing.
+ *   - all scratch is the caller's (row_logp, row_loss, work): calls with buffers of their own may overlap in time; two calls
+ *     that share `work` or an output must be ordered, or their outputs are spoiled (those of later calls are not).
  * All pointers are DEVICE.  Elements between vocab and a row's stride are neither read nor written.  dlogits may be
  * logits itself (same pointer and stride); otherwise the two must not overlap. */
 typedef enum space_dtype { SPACE_F32 = 0, SPACE_BF16 = 1 } space_dtype;
@@ -363,7 +364,9 @@ typedef struct space_loss_io {
     int32_t *n_terms;        /* [1]     rows that count                                                    */
     float *row_logp;         /* [rows]  logp of every row that counts, 0 elsewhere                         */
     float *row_loss;         /* [rows]  the rows' terms, 0 where they do not count (not used by space_preference_loss) */
-    void *work;              /* [rows * SPACE_LOSS_WORK] bytes of scratch, on 16 bytes                     */
+    void *work;              /* [(rows + 1) * SPACE_LOSS_WORK] bytes of scratch, on 16 bytes.  The first 16 (an arrival
+                                count) are cleared by the caller once, before the first call; every call leaves
+                                them as it found them.  The rest need not be cleared                        */
     int64_t logits_stride;   /* elements, >= vocab */
     int64_t dlogits_stride;
     int32_t rows;

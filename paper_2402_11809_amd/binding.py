@@ -354,7 +354,7 @@ class LossOut:
         self.n_clipped = torch.zeros(1, dtype=i32, device=dev)
         self.pair_loss = torch.zeros(pairs, dtype=f32, device=dev) if pairs else None
         self.seq_logp = torch.zeros(2 * pairs, dtype=f32, device=dev) if pairs else None
-        self.work = torch.empty(rows * SPACE_LOSS_WORK // 4, dtype=f32, device=dev)
+        self.work = torch.zeros((rows + 1) * SPACE_LOSS_WORK // 4, dtype=f32, device=dev)  # (an arrival count in front)
         self.c = SpaceLossIO(None, None, _ptr(dlogits), None, _ptr(self.loss), _ptr(self.n_terms), _ptr(self.row_logp),
                              _ptr(self.row_loss), _ptr(self.work), 0, _row_stride(dlogits), rows,
                              -1 if dlogits is None else _dtype_code(dlogits.dtype), 0)

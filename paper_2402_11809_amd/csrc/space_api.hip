@@ -584,7 +584,8 @@ int loss_launch(space_ctx* ctx, const char* who, const space_loss_io* io, bool r
     *l = LossLaunch{};
     l->logits = io->logits; l->labels = io->labels; l->dlogits = io->dlogits; l->grad_scale = io->grad_scale;
     l->loss = io->loss; l->n_terms = io->n_terms; l->row_logp = io->row_logp; l->row_loss = io->row_loss;
-    l->work = (f32x4_raw*)io->work;
+    l->arrived = (uint32_t*)io->work;  // the first 16 bytes, then 16 a row
+    l->work = (f32x4_raw*)io->work + 1;
     l->logits_stride = io->logits_stride; l->dlogits_stride = io->dlogits_stride;
     l->rows = io->rows; l->vocab = vocab; l->dtype = io->dtype; l->mean = io->mean != 0;
     l->faults = ctx->faults;

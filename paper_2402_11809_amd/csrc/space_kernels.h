@@ -369,7 +369,8 @@ struct LossLaunch {
     int32_t* n_terms;
     float* row_logp;
     float* row_loss;
-    f32x4_raw* work;  // [rows], see the kernels
+    f32x4_raw* work;    // [rows], see the kernels
+    uint32_t* arrived;  // arrival count of the rows' workgroups (space_arrivals.h), kept at 0 between calls
     int64_t logits_stride, dlogits_stride;
     int rows, vocab, dtype, mean;
     int32_t* faults;

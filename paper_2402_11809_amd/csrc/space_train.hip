@@ -60,6 +60,13 @@ __device__ __forceinline__ double block_sum(double v, double* s) {
     return v;
 }
 
+// KEPT: the ordinary way; else past the caches, for what is read once
+template <bool KEPT, typename V>
+__device__ __forceinline__ typename V::raw read_vec(const void* p) {
+    if (KEPT) return *(const typename V::raw*)p;
+    return __builtin_nontemporal_load((const typename V::raw*)p);
+}
+
 // Whether row `label` counts; one that lies behind the vocabulary is a fault of the caller's.
 __device__ __forceinline__ bool row_counts(int label, int vocab) { return label >= 0 && label < vocab; }
 
@@ -69,6 +76,150 @@ __device__ __forceinline__ void row_zero(T* __restrict__ d, int vocab) {
     const float none[V::N] = {};
     for (int i = threadIdx.x * V::N; i < vocab / V::N * V::N; i += THREADS * V::N) __builtin_nontemporal_store(V::put(none), (typename V::raw*)(d + i));
     if ((int)threadIdx.x < vocab % V::N) store_f32(d + vocab / V::N * V::N + threadIdx.x, 0.f);
+}
+
+// ---- what the rows add up to: by a launch of its own, or, where a call is small, by the rows' workgroup that ends last.  The last
+// one finds out by the caller's arrival count (space_arrivals.h); what it reads of others' rows they store past their XCD's L2.
+__device__ __forceinline__ void put(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float got(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Whether this workgroup is the last of the launch's.  Thread 0 made the row's stores.
+__device__ __forceinline__ bool rows_done(const LossLaunch& l, int* s_last) {
+    if (threadIdx.x == 0) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const uint32_t share = arrival_share(gridDim.x, blockIdx.x);
+        *s_last = arrival_is_last(__hip_atomic_fetch_add(l.arrived, share, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), share);
+    }
+    __syncthreads();
+    return *s_last;
+}
+
+// The rows that count, by a whole workgroup (without its sum over the waves): this wave's.
+template <int THREADS>
+__device__ __forceinline__ int count_rows(const LossLaunch& l) {
+    int n = 0;
+#pragma unroll 8
+    for (int r = threadIdx.x; r < l.rows; r += THREADS) n += row_counts(l.labels[r], l.vocab);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+    return n;
+}
+
+// Loss, counts: each thread adds its own rows in row order, in 64 bits, then a fixed tree.
+template <int THREADS>
+__device__ __forceinline__ void sum_rows(const LossLaunch& l, int32_t* n_clipped) {
+    constexpr int W = THREADS / 64;
+    __shared__ double s_sum[W];
+    __shared__ int2 s_n[W];
+    double sum = 0.0;
+    int n = 0, cut = 0;
+#pragma unroll 8
+    for (int r = threadIdx.x; r < l.rows; r += THREADS) {
+        sum += got(l.row_loss + r);
+        n += row_counts(l.labels[r], l.vocab);
+        if (n_clipped) cut += got(&l.work[r].v[0]) != 0.f;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        sum += __shfl_xor(sum, o, 64);
+        n += __shfl_xor(n, o, 64);
+        cut += __shfl_xor(cut, o, 64);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        s_sum[threadIdx.x >> 6] = sum;
+        s_n[threadIdx.x >> 6] = int2{n, cut};
+    }
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < W; ++w) {
+        sum += s_sum[w];
+        n += s_n[w].x;
+        cut += s_n[w].y;
+    }
+    *l.loss = (float)(l.mean ? sum / max(n, 1) : sum);
+    *l.n_terms = n;
+    if (n_clipped) *n_clipped = cut;
+}
+
+// The pairs, a sequence to a wave: sums over the rows of both sequences, the pair's term, and the slope of every row.
+template <int THREADS>
+__device__ __forceinline__ void join_pairs(const LossLaunch& l, const PrefArgs& p) {
+    constexpr int W = THREADS / 64, P = W > 1 ? W / 2 : 1;  // pairs at a time
+    __shared__ double s_sum[2 * P], s_term[P];
+    __shared__ int s_n[2 * P];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    double all = 0.0;
+    int n_all = 0;
+    if (l.dlogits) {  // rows of no sequence
+        for (int r = threadIdx.x; r < l.rows; r += THREADS) l.work[r].v[3] = 0.f;
+        __syncthreads();
+    }
+    for (int first = 0; first < p.pairs; first += P) {
+        int from[2] = {}, to[2] = {};
+        // (a lone wave has both sequences of a pair in turn)
+        const int turns = W > 1 ? 1 : 2;
+#pragma unroll
+        for (int k = 0; k < turns; ++k) {
+            const int at = W > 1 ? wave : k, seq = 2 * first + at;
+            if (seq >= 2 * p.pairs) break;
+            const int a = p.seq_start[seq], b = p.seq_start[seq + 1];
+            from[k] = min(max(a, 0), l.rows);
+            to[k] = min(max(b, from[k]), l.rows);
+            if (lane == 0 && (a != from[k] || b != to[k])) atomicAdd(l.faults, 1);
+            double t = 0.0;
+            int n = 0;
+#pragma unroll 8
+            for (int r = from[k] + lane; r < to[k]; r += 64) {
+                t += got(l.row_logp + r);
+                n += row_counts(l.labels[r], l.vocab);
+            }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) {
+                t += __shfl_xor(t, o, 64);
+                n += __shfl_xor(n, o, 64);
+            }
+            if (p.average) t /= max(n, 1);
+            if (lane == 0) {
+                s_sum[at] = p.ref_logp ? t - p.ref_logp[seq] : t;
+                s_n[at] = n;
+                if (p.seq_logp) p.seq_logp[seq] = (float)t;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < turns; ++k) {
+            const int at = W > 1 ? wave : k, pair = first + at / 2;
+            if (pair >= p.pairs) break;
+            const double z = (double)p.beta * (s_sum[at & ~1] - s_sum[at | 1]) - (double)p.margin, eps = p.smoothing;
+            const double far = exp(-fabs(z)), tail = log1p(far);
+            if (lane == 0 && at % 2 == 0) {
+                const double low = fmax(-z, 0.0) + tail, high = fmax(z, 0.0) + tail;  // softplus(-z), softplus(z)
+                const double term = (eps < 1.0 ? (1.0 - eps) * low : 0.0) + (eps > 0.0 ? eps * high : 0.0);
+                p.pair_loss[pair] = (float)term;
+                s_term[at / 2] = term;
+            }
+            if (!l.dlogits) continue;
+            // sigmoid(z) and sigmoid(-z), each without a difference from 1
+            const double big = 1.0 / (1.0 + far), small = far / (1.0 + far);
+            double c = (double)p.beta * (eps * (z >= 0.0 ? big : small) - (1.0 - eps) * (z >= 0.0 ? small : big));
+            if (l.mean) c /= p.pairs;
+            if (l.grad_scale) c *= *l.grad_scale;
+            if (p.average) c /= max(s_n[at], 1);
+            const float slope = (float)(at % 2 ? -c : c);
+            for (int r = from[k] + lane; r < to[k]; r += 64) l.work[r].v[3] = slope;
+        }
+        __syncthreads();
+        if (threadIdx.x == 0)
+            for (int k = 0; k < P && first + k < p.pairs; ++k) {
+                all += s_term[k];
+                n_all += s_n[2 * k] + s_n[2 * k + 1];
+            }
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        *l.loss = (float)(l.mean ? all / p.pairs : all);
+        *l.n_terms = n_all;
+    }
 }
 
 // What a row's label and its other tokens add up to, in the row's own scale (its maximum)
@@ -104,6 +255,14 @@ __device__ __forceinline__ RowFacts join_waves(float mx, double sum, float x_lab
     return f;
 }
 
+template <int W>
+__device__ __forceinline__ int sum_of(const int* s) {
+    int n = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) n += s[w];
+    return n;
+}
+
 struct RowSlope {
     double term, slope, kl;
     bool clipped;
@@ -137,10 +296,10 @@ __device__ __forceinline__ RowSlope row_slope(const PolicyArgs& p, int row, doub
 template <typename T, int KIND, int THREADS>
 __device__ __forceinline__ void row_left_out(const LossLaunch& l, const PolicyArgs& p, int row, int label, T* d) {
     if (threadIdx.x == 0) {
-        l.row_logp[row] = 0.f;
-        if (KIND != LOSS_PREF) l.row_loss[row] = 0.f;
+        put(l.row_logp + row, 0.f);
+        if (KIND != LOSS_PREF) put(l.row_loss + row, 0.f);
         if (KIND == LOSS_POLICY && p.row_kl) p.row_kl[row] = 0.f;
-        l.work[row] = f32x4_raw{{0.f, 0.f, 0.f, 0.f}};
+        if (KIND == LOSS_POLICY) put(&l.work[row].v[0], 0.f);
         if (label >= 0) atomicAdd(l.faults, 1);
     }
     if (KIND != LOSS_PREF && d) row_zero<T, THREADS>(d, l.vocab);
@@ -150,32 +309,43 @@ __device__ __forceinline__ void row_left_out(const LossLaunch& l, const PolicyAr
 template <int KIND>
 __device__ __forceinline__ double row_outputs(const LossLaunch& l, const PolicyArgs& p, int row, const RowFacts& f, float x_label) {
     const double logp = f.logp(x_label);
-    l.row_logp[row] = (float)logp;
-    if (KIND == LOSS_PREF) {
-        l.work[row] = f32x4_raw{{f.top, (float)(1.0 / f.total), (float)(f.others / f.total), 0.f}};
+    put(l.row_logp + row, (float)logp);
+    if (KIND == LOSS_PREF) {  // (behind them stands the row's slope, which join_pairs writes)
+        l.work[row].v[0] = f.top;
+        l.work[row].v[1] = (float)(1.0 / f.total);
+        l.work[row].v[2] = (float)(f.others / f.total);
         return 0.0;
     }
     const RowSlope s = row_slope<KIND>(p, row, logp);
-    l.row_loss[row] = (float)s.term;
+    put(l.row_loss + row, (float)s.term);
     if (KIND == LOSS_POLICY) {
-        l.work[row] = f32x4_raw{{s.clipped ? 1.f : 0.f, 0.f, 0.f, 0.f}};
+        put(&l.work[row].v[0], s.clipped ? 1.f : 0.f);
         if (p.row_kl) p.row_kl[row] = (float)s.kl;
     }
     return s.slope;
 }
 // What the gradient of the loss along logp is multiplied with.
-__device__ __forceinline__ double slope_factor(const LossLaunch& l) {
-    double c = l.mean ? 1.0 / max(*l.n_terms, 1) : 1.0;
+__device__ __forceinline__ double slope_factor(const LossLaunch& l, int n) {
+    double c = l.mean ? 1.0 / max(n, 1) : 1.0;
     if (l.grad_scale) c *= *l.grad_scale;
     return c;
 }
 // The slope with everything in it, for all threads; the policy loss has it from thread 0.
 template <int KIND>
-__device__ __forceinline__ float row_coefficient(const LossLaunch& l, const PolicyArgs& p, int row, const RowFacts& f, float x_label, float* s_slope) {
-    if (KIND == LOSS_SAR) return (float)-slope_factor(l);
-    if (threadIdx.x == 0) *s_slope = (float)(row_outputs<KIND>(l, p, row, f, x_label) * slope_factor(l));
+__device__ __forceinline__ float row_coefficient(const LossLaunch& l, const PolicyArgs& p, int row, const RowFacts& f, float x_label, int n, float* s_slope) {
+    if (KIND == LOSS_SAR) return (float)-slope_factor(l, n);
+    if (threadIdx.x == 0) *s_slope = (float)(row_outputs<KIND>(l, p, row, f, x_label) * slope_factor(l, n));
     __syncthreads();
     return *s_slope;
+}
+
+// Behind a row: the last workgroup adds up.
+template <int KIND, int THREADS>
+__device__ __forceinline__ void finish_rows(const LossLaunch& l, const PolicyArgs& p, const PrefArgs& pref) {
+    __shared__ int s_last;
+    if (!rows_done(l, &s_last)) return;
+    if (KIND == LOSS_PREF) join_pairs<THREADS>(l, pref);
+    else sum_rows<THREADS>(l, p.n_clipped);
 }
 
 // A row in the registers of one workgroup: read once, written once.  Bound by memory: a row that is read while another one
@@ -185,12 +355,13 @@ __device__ __forceinline__ float row_coefficient(const LossLaunch& l, const Poli
 // 5.77 TB/s read and written in fp32 (4096 rows of 32000, 182 us), 5.46 in bf16 (8192 rows, 192 us), where a copy of such
 // buffers reaches 4.8 - 4.9; all in one launch of 1024 threads and 32 elements 5.0 and 4.0.  Loads and stores are non-temporal:
 // stores 5.1 -> 5.5 TB/s.
-template <typename T, int KIND, int THREADS, int NV, bool KEEP>
-__global__ __launch_bounds__(THREADS, 4) void loss_rows_kernel(LossLaunch l, PolicyArgs p) {
+template <typename T, int KIND, int THREADS, int NV, bool KEEP, bool SMALL>
+__device__ __forceinline__ void row_of_loss(const LossLaunch& l, const PolicyArgs& p) {
     typedef Vec<T> V;
     constexpr int W = THREADS / 64, E = V::N;
     __shared__ float s_max[W], s_slope;
     __shared__ double s_sum[W];
+    __shared__ int s_n[W];
     const int row = blockIdx.x, tid = threadIdx.x, label = l.labels[row], vocab = l.vocab;
     const T* x = (const T*)l.logits + (size_t)row * l.logits_stride;
     T* d = l.dlogits ? (T*)l.dlogits + (size_t)row * l.dlogits_stride : nullptr;
@@ -201,7 +372,7 @@ __global__ __launch_bounds__(THREADS, 4) void loss_rows_kernel(LossLaunch l, Pol
     typename V::raw q[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-        if (tid + j * THREADS < whole) q[j] = __builtin_nontemporal_load((const typename V::raw*)(x + (size_t)(tid + j * THREADS) * E));
+        if (tid + j * THREADS < whole) q[j] = read_vec<KIND == LOSS_PREF, V>(x + (size_t)(tid + j * THREADS) * E);
     float t = odd < vocab && odd != label ? load_f32(x + odd) : -INFINITY;
     float v[KEEP ? NV * E : E], mx = t;
     // vector j as 32-bit numbers, nothing behind the row and nothing at the label, which stands apart
@@ -247,13 +418,19 @@ __global__ __launch_bounds__(THREADS, 4) void loss_rows_kernel(LossLaunch l, Pol
     double sum = ((double)part[0] + part[1]) + ((double)part[2] + part[3]) + t;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    // the mean's divisor: counted here in a small call, by a launch in front in a large one
+    if (SMALL && KIND != LOSS_PREF && l.mean && d) {
+        const int n = count_rows<THREADS>(l);
+        if ((tid & 63) == 0) s_n[tid >> 6] = n;
+    }
     float factor;
     const RowFacts f = join_waves<W>(mx, sum, x_label, &factor, s_max, s_sum);
     if (KIND == LOSS_PREF || !d) {
         if (tid == 0) row_outputs<KIND>(l, p, row, f, x_label);
         return;
     }
-    const float c = row_coefficient<KIND>(l, p, row, f, x_label, &s_slope);
+    const int n = !l.mean ? 1 : SMALL ? sum_of<W>(s_n) : *l.n_terms;
+    const float c = row_coefficient<KIND>(l, p, row, f, x_label, n, &s_slope);
     const float inv = 1.f / (float)f.total, per_e = -c * inv * factor, at_label = c * ((float)f.others / (float)f.total);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -278,21 +455,27 @@ __global__ __launch_bounds__(THREADS, 4) void loss_rows_kernel(LossLaunch l, Pol
     if (KIND == LOSS_SAR && tid == 0) row_outputs<KIND>(l, p, row, f, x_label);
 }
 
+template <typename T, int KIND, int THREADS, int NV, bool KEEP, bool SMALL>
+__global__ __launch_bounds__(THREADS, 4) void loss_rows_kernel(LossLaunch l, PolicyArgs p, PrefArgs pref) {
+    row_of_loss<T, KIND, THREADS, NV, KEEP, SMALL>(l, p);
+    if (SMALL) finish_rows<KIND, THREADS>(l, p, pref);
+}
+
 // A row that no workgroup's registers hold: once for maximum and sum, once for the gradient.
 constexpr int kLongThreads = 1024, kLongVecs = 4;
-template <typename T>
+template <typename T, int THREADS>
 __device__ __forceinline__ void long_gradient(const T* x, T* d, int vocab, int label, float top, float per_e, float at_label) {
     typedef Vec<T> V;
     constexpr int E = V::N;
     const int whole = vocab / E, odd = whole * E + threadIdx.x;
-    for (int at = threadIdx.x; at < whole; at += kLongThreads * kLongVecs) {
+    for (int at = threadIdx.x; at < whole; at += THREADS * kLongVecs) {
         typename V::raw q[kLongVecs];
 #pragma unroll
         for (int j = 0; j < kLongVecs; ++j)
-            if (at + j * kLongThreads < whole) q[j] = *(const typename V::raw*)(x + (size_t)(at + j * kLongThreads) * E);
+            if (at + j * THREADS < whole) q[j] = *(const typename V::raw*)(x + (size_t)(at + j * THREADS) * E);
 #pragma unroll
         for (int j = 0; j < kLongVecs; ++j) {
-            const int i = at + j * kLongThreads;
+            const int i = at + j * THREADS;
             if (i >= whole) break;
             float g[E];
             V::get(q[j], g);
@@ -309,12 +492,13 @@ __device__ __forceinline__ void long_gradient(const T* x, T* d, int vocab, int l
     if (odd < vocab) store_f32(d + odd, odd == label ? at_label : per_e * exp_below(load_f32(x + odd) - top));
 }
 
-template <typename T, int KIND>
-__global__ __launch_bounds__(kLongThreads) void loss_long_rows_kernel(LossLaunch l, PolicyArgs p) {
+template <typename T, int KIND, bool SMALL>
+__device__ __forceinline__ void long_row_of_loss(const LossLaunch& l, const PolicyArgs& p) {
     typedef Vec<T> V;
     constexpr int W = kLongThreads / 64, E = V::N;
     __shared__ float s_max[W], s_slope;
     __shared__ double s_sum[W];
+    __shared__ int s_n[W];
     const int row = blockIdx.x, tid = threadIdx.x, label = l.labels[row], vocab = l.vocab;
     const T* x = (const T*)l.logits + (size_t)row * l.logits_stride;
     T* d = l.dlogits ? (T*)l.dlogits + (size_t)row * l.dlogits_stride : nullptr;
@@ -360,145 +544,118 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_rows_kernel(LossLaunch
     if (mx != -INFINITY) sum *= exp_below(mx - top);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    // the mean's divisor: counted here in a small call, by a launch in front in a large one
+    if (SMALL && KIND != LOSS_PREF && l.mean && d) {
+        const int n = count_rows<kLongThreads>(l);
+        if ((tid & 63) == 0) s_n[tid >> 6] = n;
+    }
     float factor;
     const RowFacts f = join_waves<W>(top, sum, x_label, &factor, s_max, s_sum);
     if (KIND == LOSS_PREF || !d) {
         if (tid == 0) row_outputs<KIND>(l, p, row, f, x_label);
         return;
     }
-    const float c = row_coefficient<KIND>(l, p, row, f, x_label, &s_slope);
+    const int n = !l.mean ? 1 : SMALL ? sum_of<W>(s_n) : *l.n_terms;
+    const float c = row_coefficient<KIND>(l, p, row, f, x_label, n, &s_slope);
     const float inv = 1.f / (float)f.total;
-    long_gradient(x, d, vocab, label, f.top, -c * inv, c * ((float)f.others / (float)f.total));
+    long_gradient<T, kLongThreads>(x, d, vocab, label, f.top, -c * inv, c * ((float)f.others / (float)f.total));
     if (KIND == LOSS_SAR && tid == 0) row_outputs<KIND>(l, p, row, f, x_label);
+}
+
+template <typename T, int KIND, bool SMALL>
+__global__ __launch_bounds__(kLongThreads) void loss_long_rows_kernel(LossLaunch l, PolicyArgs p, PrefArgs pref) {
+    long_row_of_loss<T, KIND, SMALL>(l, p);
+    if (SMALL) finish_rows<KIND, kLongThreads>(l, p, pref);
 }
 
 // How many rows count, for the mean that the rows' gradients need before the rows are done.
 __global__ __launch_bounds__(1024) void loss_count_kernel(LossLaunch l) {
-    __shared__ double s[16];
-    int n = 0;
-    for (int r = threadIdx.x; r < l.rows; r += 1024) n += row_counts(l.labels[r], l.vocab);
-    const double all = block_sum<16>(n, s);
-    if (threadIdx.x == 0) *l.n_terms = (int)all;
+    __shared__ int s[16];
+    const int n = count_rows<1024>(l);
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = n;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    int all = 0;
+    for (int w = 0; w < 16; ++w) all += s[w];
+    *l.n_terms = all;
 }
+__global__ __launch_bounds__(1024) void loss_sum_kernel(LossLaunch l, int32_t* n_clipped) { sum_rows<1024>(l, n_clipped); }
+__global__ __launch_bounds__(1024) void pref_pairs_kernel(LossLaunch l, PrefArgs p) { join_pairs<1024>(l, p); }
 
-// The rows' terms added up: each thread its own in row order, then a fixed tree, in 64 bits.
-__global__ __launch_bounds__(1024) void loss_sum_kernel(LossLaunch l, int32_t* n_clipped) {
-    __shared__ double s[16];
-    double sum = 0.0;
-    int n = 0, clipped = 0;
-    for (int r = threadIdx.x; r < l.rows; r += 1024) {
-        sum += l.row_loss[r];
-        n += row_counts(l.labels[r], l.vocab);
-        if (n_clipped) clipped += l.work[r].v[0] != 0.f;
-    }
-    sum = block_sum<16>(sum, s);
-    const double count = block_sum<16>(n, s);
-    const double cut = n_clipped ? block_sum<16>(clipped, s) : 0.0;
-    if (threadIdx.x == 0) {
-        *l.loss = (float)(l.mean ? sum / fmax(count, 1.0) : sum);
-        *l.n_terms = (int)count;
-        if (n_clipped) *n_clipped = (int)cut;
-    }
-}
-
-// The pairs, one to a wave: sums over the rows of their two sequences, their terms, and the slope of every row.
-__global__ __launch_bounds__(1024) void pref_pairs_kernel(LossLaunch l, PrefArgs p) {
-    __shared__ double s[16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    double sum = 0.0;
-    int n_all = 0;
-    for (int pair = wave; pair < p.pairs; pair += 16) {
-        int from[2], to[2], n[2];
-        double ratio[2];
-        bool bad = false;
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            const int a = p.seq_start[2 * pair + w], b = p.seq_start[2 * pair + w + 1];
-            from[w] = min(max(a, 0), l.rows);
-            to[w] = min(max(b, from[w]), l.rows);
-            bad = bad || a != from[w] || b != to[w];
-            double t = 0.0;
-            int k = 0;
-            for (int r = from[w] + lane; r < to[w]; r += 64) {
-                t += l.row_logp[r];
-                k += row_counts(l.labels[r], l.vocab);
-            }
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) {
-                t += __shfl_xor(t, o, 64);
-                k += __shfl_xor(k, o, 64);
-            }
-            if (p.average) t /= max(k, 1);
-            n[w] = k;
-            n_all += k;
-            if (lane == 0 && p.seq_logp) p.seq_logp[2 * pair + w] = (float)t;
-            ratio[w] = p.ref_logp ? t - p.ref_logp[2 * pair + w] : t;
-        }
-        if (bad && lane == 0) atomicAdd(l.faults, 1);
-        const double z = (double)p.beta * (ratio[0] - ratio[1]) - (double)p.margin, eps = p.smoothing;
-        const double tail = log1p(exp(-fabs(z))), low = fmax(-z, 0.0) + tail, high = fmax(z, 0.0) + tail;  // softplus(-z), softplus(z)
-        const double term = (eps < 1.0 ? (1.0 - eps) * low : 0.0) + (eps > 0.0 ? eps * high : 0.0);
-        if (lane == 0) p.pair_loss[pair] = (float)term;
-        sum += term;
-        if (!l.dlogits) continue;
-        // sigmoid(z) and sigmoid(-z), each without a difference from 1
-        const double t = exp(-fabs(z)), big = 1.0 / (1.0 + t), small = t / (1.0 + t);
-        double slope = (double)p.beta * (eps * (z >= 0.0 ? big : small) - (1.0 - eps) * (z >= 0.0 ? small : big));
-        if (l.mean) slope /= p.pairs;
-        if (l.grad_scale) slope *= *l.grad_scale;
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            const double c = (w ? -slope : slope) / (p.average ? max(n[w], 1) : 1);
-            for (int r = from[w] + lane; r < to[w]; r += 64) l.work[r].v[3] = (float)c;
-        }
-    }
-    sum = block_sum<16>(lane == 0 ? sum : 0.0, s);
-    const double n = block_sum<16>(lane == 0 ? n_all : 0, s);
-    if (threadIdx.x == 0) {
-        *l.loss = (float)(l.mean ? sum / p.pairs : sum);
-        *l.n_terms = (int)n;
-    }
-}
-
-template <typename T>
-__global__ __launch_bounds__(kLongThreads) void pref_gradient_kernel(LossLaunch l) {
-    const int row = blockIdx.x, label = l.labels[row];
+// The gradient of the preference loss, a row to a workgroup.  A row's coefficient is known when its whole pair has been read, so the
+// logits are read twice; the last rows first, which the memory-side cache still holds from the first time (7264 rows of 32000 in
+// bf16, six in ten counting: both passes 197 -> 171 us).
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void pref_gradient_kernel(LossLaunch l) {
+    const int row = l.rows - 1 - blockIdx.x, label = l.labels[row];
     T* d = (T*)l.dlogits + (size_t)row * l.dlogits_stride;
     const f32x4_raw f = l.work[row];
-    if (!row_counts(label, l.vocab) || f.v[3] == 0.f) return row_zero<T, kLongThreads>(d, l.vocab);
-    long_gradient((const T*)l.logits + (size_t)row * l.logits_stride, d, l.vocab, label, f.v[0], -f.v[3] * f.v[1], f.v[3] * f.v[2]);
+    if (!row_counts(label, l.vocab) || f.v[3] == 0.f) return row_zero<T, THREADS>(d, l.vocab);
+    long_gradient<T, THREADS>((const T*)l.logits + (size_t)row * l.logits_stride, d, l.vocab, label, f.v[0], -f.v[3] * f.v[1], f.v[3] * f.v[2]);
+}
+template <typename T>
+hipError_t launch_pref_gradient(const LossLaunch& l, hipStream_t s) {
+    const dim3 grid(l.rows);
+    if (l.vocab <= 64 * 32) hipLaunchKernelGGL((pref_gradient_kernel<T, 64>), grid, dim3(64), 0, s, l);
+    else if (l.vocab <= 256 * 32) hipLaunchKernelGGL((pref_gradient_kernel<T, 256>), grid, dim3(256), 0, s, l);
+    else hipLaunchKernelGGL((pref_gradient_kernel<T, 1024>), grid, dim3(1024), 0, s, l);
+    return hipGetLastError();
 }
 
-template <typename T, int KIND>
-hipError_t launch_rows_of(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) {
+template <typename T, int KIND, bool SMALL>
+hipError_t launch_rows_of(const LossLaunch& l, const PolicyArgs& p, const PrefArgs& pref, hipStream_t s) {
     constexpr int E = Vec<T>::N;
     const dim3 grid(l.rows);
 #define SPACE_ROWS(THREADS, ELEMS, KEEP) \
-    hipLaunchKernelGGL((loss_rows_kernel<T, KIND, THREADS, ELEMS / E, KEEP>), grid, dim3(THREADS), 0, s, l, p)
-    if (l.vocab <= 64 * 32) SPACE_ROWS(64, 32, true);
-    else if (l.vocab <= 128 * 32) SPACE_ROWS(128, 32, true);
-    else if (l.vocab <= 128 * 64) SPACE_ROWS(128, 64, true);
-    else if (l.vocab <= 256 * 64) SPACE_ROWS(256, 64, true);
-    else if (l.vocab <= 512 * 64) SPACE_ROWS(512, 64, true);
-    else if (sizeof(T) == 4 && l.vocab <= 1024 * 64) SPACE_ROWS(1024, 64, true);
-    else if (sizeof(T) == 2 && l.vocab <= 512 * 128) SPACE_ROWS(512, sizeof(T) == 2 ? 128 : 64, false);
-    else if (sizeof(T) == 2 && l.vocab <= 1024 * 128) SPACE_ROWS(1024, sizeof(T) == 2 ? 128 : 64, false);
-    else hipLaunchKernelGGL((loss_long_rows_kernel<T, KIND>), grid, dim3(kLongThreads), 0, s, l, p);
+    hipLaunchKernelGGL((loss_rows_kernel<T, KIND, THREADS, (ELEMS) / E, KEEP, SMALL>), grid, dim3(THREADS), 0, s, l, p, pref)
+    if (l.vocab <= 64 * 32) {
+        SPACE_ROWS(64, 32, true);
+    } else if (l.vocab <= 128 * 32) {
+        SPACE_ROWS(128, 32, true);
+    } else if (l.vocab <= 128 * 64) {
+        SPACE_ROWS(128, 64, true);
+    } else if (l.vocab <= 256 * 64) {
+        SPACE_ROWS(256, 64, true);
+    } else if (l.vocab <= 512 * 64) {
+        SPACE_ROWS(512, 64, true);
+    } else {
+        if constexpr (sizeof(T) == 4) {
+            if (l.vocab <= 1024 * 64) {
+                SPACE_ROWS(1024, 64, true);
+                return hipGetLastError();
+            }
+        } else {
+            if (l.vocab <= 512 * 128) {
+                SPACE_ROWS(512, 128, false);
+                return hipGetLastError();
+            } else if (KIND != LOSS_PREF && l.vocab <= 1024 * 128) {
+                SPACE_ROWS(1024, 128, false);
+                return hipGetLastError();
+            }
+        }
+        hipLaunchKernelGGL((loss_long_rows_kernel<T, KIND, SMALL>), grid, dim3(kLongThreads), 0, s, l, p, pref);
+    }
 #undef SPACE_ROWS
     return hipGetLastError();
 }
 template <int KIND>
-hipError_t launch_rows(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) {
-    return l.dtype == 0 ? launch_rows_of<float, KIND>(l, p, s) : launch_rows_of<uint16_t, KIND>(l, p, s);
+hipError_t launch_rows(const LossLaunch& l, const PolicyArgs& p, const PrefArgs& pref, bool small, hipStream_t s) {
+    if (l.dtype == 0) return small ? launch_rows_of<float, KIND, true>(l, p, pref, s) : launch_rows_of<float, KIND, false>(l, p, pref, s);
+    return small ? launch_rows_of<uint16_t, KIND, true>(l, p, pref, s) : launch_rows_of<uint16_t, KIND, false>(l, p, pref, s);
 }
+
+// Whether the rows' workgroups count and add up themselves.  That saves two launches (about 6 us of 15), but every workgroup reads
+// all labels and adds to one count.
+bool small_call(const LossLaunch& l) { return l.rows <= 2048 && (int64_t)l.rows * 4 <= (int64_t)l.vocab * (l.dtype ? 2 : 4) / 8; }
 
 template <int KIND>
 hipError_t launch_loss(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) {
+    if (small_call(l)) return launch_rows<KIND>(l, p, PrefArgs{}, true, s);
     if (l.mean && l.dlogits) {
         hipLaunchKernelGGL(loss_count_kernel, dim3(1), dim3(1024), 0, s, l);
         if (hipError_t e = hipGetLastError()) return e;
     }
-    if (hipError_t e = launch_rows<KIND>(l, p, s)) return e;
+    if (hipError_t e = launch_rows<KIND>(l, p, PrefArgs{}, false, s)) return e;
     hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, s, l, p.n_clipped);
     return hipGetLastError();
 }
@@ -507,13 +664,14 @@ hipError_t launch_sar_grad(const LossLaunch& l, hipStream_t s) { return launch_l
 hipError_t launch_policy(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) { return launch_loss<LOSS_POLICY>(l, p, s); }
 
 hipError_t launch_preference(const LossLaunch& l, const PrefArgs& p, hipStream_t s) {
-    if (hipError_t e = launch_rows<LOSS_PREF>(l, PolicyArgs{}, s)) return e;
-    hipLaunchKernelGGL(pref_pairs_kernel, dim3(1), dim3(1024), 0, s, l, p);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !l.dlogits) return e;
-    if (l.dtype == 0) hipLaunchKernelGGL(pref_gradient_kernel<float>, dim3(l.rows), dim3(kLongThreads), 0, s, l);
-    else hipLaunchKernelGGL(pref_gradient_kernel<uint16_t>, dim3(l.rows), dim3(kLongThreads), 0, s, l);
-    return hipGetLastError();
+    const bool small = small_call(l);
+    if (hipError_t e = launch_rows<LOSS_PREF>(l, PolicyArgs{}, p, small, s)) return e;
+    if (!small) {
+        hipLaunchKernelGGL(pref_pairs_kernel, dim3(1), dim3(1024), 0, s, l, p);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    if (!l.dlogits) return hipSuccess;
+    return l.dtype == 0 ? launch_pref_gradient<float>(l, s) : launch_pref_gradient<uint16_t>(l, s);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -545,12 +703,6 @@ __device__ __forceinline__ int grad_tensor_of(const GradList& g, int64_t chunk) 
 // last kGradKept bytes are read in the ordinary way by the norm, and first by the clipping; everything in front of them, which the
 // cache would lose again, is read past it.
 constexpr int64_t kGradKept = 192ll << 20;
-template <bool KEPT, typename V>
-__device__ __forceinline__ typename V::raw read_grad(const void* p) {
-    if (KEPT) return *(const typename V::raw*)p;
-    return __builtin_nontemporal_load((const typename V::raw*)p);
-}
-
 // The squares of n elements of a chunk, this thread's share.  A square is exact in 64 bits for both types, and no sum of them leaves the range.
 template <typename T, bool KEPT>
 __device__ __forceinline__ double chunk_squares(const T* __restrict__ x, int n) {
@@ -561,7 +713,7 @@ __device__ __forceinline__ double chunk_squares(const T* __restrict__ x, int n) 
     if (n == kGradChunk) {
         typename V::raw q[NV];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) q[j] = read_grad<KEPT, V>(x + (tid + j * kGradThreads) * E);
+        for (int j = 0; j < NV; ++j) q[j] = read_vec<KEPT, V>(x + (tid + j * kGradThreads) * E);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             float v[E];
@@ -610,13 +762,13 @@ __global__ __launch_bounds__(1024) void grad_norm_kernel(const double* work, int
 
 // N elements as a thread reads or writes them: 16 bytes, or 8 where bf16 goes with fp32, so that neighbouring lanes' stores meet
 template <typename T, int N> struct Some {
-    template <bool KEPT> static __device__ __forceinline__ void load(const T* p, float* v) { Vec<T>::get(read_grad<KEPT, Vec<T>>(p), v); }
+    template <bool KEPT> static __device__ __forceinline__ void load(const T* p, float* v) { Vec<T>::get(read_vec<KEPT, Vec<T>>(p), v); }
     static __device__ __forceinline__ void store(T* p, const float* v) { __builtin_nontemporal_store(Vec<T>::put(v), (typename Vec<T>::raw*)p); }
 };
 template <> struct Some<uint16_t, 4> {
     typedef uint32_t raw __attribute__((ext_vector_type(2), aligned(2)));
     template <bool KEPT> static __device__ __forceinline__ void load(const uint16_t* p, float* v) {
-        const raw q = read_grad<KEPT, Some>(p);
+        const raw q = read_vec<KEPT, Some>(p);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const uint32_t w = q[e];

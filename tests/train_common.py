@@ -92,8 +92,9 @@ def spoil(t):
 def fresh_out(gm, rows, dtype=None, **kw):
     from paper_2402_11809_amd import binding
     out = binding.LossOut(gm, rows, grad_dtype=None if dtype is None else torch_type(dtype), **kw)
-    for n in ("loss", "n_terms", "row_logp", "row_loss", "row_kl", "n_clipped", "pair_loss", "seq_logp", "work", "dlogits"):
+    for n in ("loss", "n_terms", "row_logp", "row_loss", "row_kl", "n_clipped", "pair_loss", "seq_logp", "dlogits"):
         t = getattr(out, n)
         if t is not None and "dlogits" not in kw:
             spoil(t)
+    spoil(out.work[4:])  # (an arrival count in front)
     return out
