@@ -377,8 +377,8 @@ typedef struct space_loss_io {
 #define SPACE_LOSS_WORK 16 /* bytes a row */
 
 /* The loss of space_sar_loss with its gradient: term_r = -logp_r.  Asynchronous on `stream`, no allocation.
- * Errors of all three: SPACE_EINVAL (null pointer, rows < 1, stride below vocab, unknown dtype, dlogits overlapping logits,
- * a parameter out of its range). */
+ * Errors of all three: SPACE_EINVAL (null pointer, rows < 1, stride below vocab, unknown dtype, an array that is not on its
+ * element's size, dlogits overlapping logits, a parameter out of its range), SPACE_ESHAPE (rows or pairs >= 4194304). */
 int space_sar_loss_grad(space_ctx *ctx, const space_loss_io *io, void *stream);
 
 /* Clipped policy loss with a KL term, for rollouts of this model (labels = the tokens that were generated):
@@ -428,11 +428,13 @@ typedef struct space_grad_tensor {
     int32_t dtype;     /* space_dtype */
     int32_t out_dtype;
 } space_grad_tensor;
-#define SPACE_GRAD_WORK 2048 /* doubles of scratch */
+#define SPACE_GRAD_WORK 2050 /* doubles of scratch */
 
 /* *norm = sqrt(sum of squares), squares and sums in 64 bits (no overflow in between) and in an order that depends on the
  * tensors' lengths and types alone.  n_tensors == 0 gives 0.  `out` is not looked at.
- *   norm  DEVICE float32 [1];   work  DEVICE float64 [SPACE_GRAD_WORK], overwritten
+ *   norm  DEVICE float32 [1]
+ *   work  DEVICE float64 [SPACE_GRAD_WORK], the caller's: the first 16 bytes (an arrival count) are cleared once, before the first
+ *         call, and left as they were by every call; the rest is scratch.  Calls that share it must be ordered
  * Errors: SPACE_EINVAL (null, negative length, unknown dtype, pointer that is not on a whole element). */
 int space_grad_norm(space_ctx *ctx, const space_grad_tensor *tensors, int32_t n_tensors, float *norm, double *work, void *stream);
 

@@ -101,7 +101,7 @@ class SpaceGradTensor(C.Structure):
 
 SPACE_F32, SPACE_BF16 = 0, 1
 SPACE_LOSS_WORK = 16    # bytes of scratch a row of logits
-SPACE_GRAD_WORK = 2048  # doubles
+SPACE_GRAD_WORK = 2050  # doubles
 
 
 def library_path() -> str:
@@ -382,7 +382,7 @@ class GradSet:
             assert g.shape == o.shape and (g is o or _same_order(g, o)), f"tensor {i}: gradient and output laid out differently"
             self.c[i] = SpaceGradTensor(_ptr(g), _ptr(o), g.numel(), _dtype_code(g.dtype), _dtype_code(o.dtype))
         self.norm = torch.zeros(1, dtype=torch.float32, device=model.device)
-        self.work = torch.empty(SPACE_GRAD_WORK, dtype=torch.float64, device=model.device)
+        self.work = torch.zeros(SPACE_GRAD_WORK, dtype=torch.float64, device=model.device)  # (an arrival count in front)
 
 
 def _dense(t) -> bool:
@@ -541,7 +541,9 @@ class Model:
             assert grad_scale.dtype is torch.float32 and grad_scale.device == self.device and grad_scale.numel() == 1
         io = out.c
         code = _dtype_code(logits.dtype)
-        assert out.dlogits is None or out.dlogits.dtype == logits.dtype, "dlogits has the type of the logits"
+        if out.dlogits is not None:
+            assert out.dlogits.dtype == logits.dtype, "dlogits has the type of the logits"
+            assert out.dlogits.shape[1] == self.cfg.vocab and out.dlogits.device == self.device
         io.logits, io.labels, io.grad_scale = logits.data_ptr(), labels.data_ptr(), _ptr(grad_scale)
         io.logits_stride, io.dtype, io.mean = _row_stride(logits), code, int(bool(mean))
         return io
@@ -598,8 +600,9 @@ class Model:
         import torch
         if norm is None:
             norm = self.grad_norm(grads, stream)
-        assert grads.model is self and torch.cuda.current_device() == self.device.index
-        assert norm.dtype is torch.float32 and norm.numel() == 1 and norm.device == self.device
+        else:
+            assert grads.model is self and torch.cuda.current_device() == self.device.index
+            assert norm.dtype is torch.float32 and norm.numel() == 1 and norm.device == self.device
         self._check(self.lib.space_grad_clip(self.ctx, grads.c, len(grads.grads), norm.data_ptr(), float(max_norm), _stream(stream)))
         return norm
 

@@ -8,6 +8,7 @@
 #include <cstdlib>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 #include <map>
@@ -563,6 +564,14 @@ namespace {
 
 size_t dtype_bytes(int dtype) { return dtype == SPACE_F32 ? 4 : dtype == SPACE_BF16 ? 2 : 0; }
 
+constexpr int kLossRows = (1 << 22) - 1;  // a launch has fewer than 2^32 threads, a row up to 1024
+
+bool words(std::initializer_list<const void*> ptrs) {  // on 4 bytes (or null)
+    for (const void* p : ptrs)
+        if ((uintptr_t)p % 4) return false;
+    return true;
+}
+
 // The checks that the losses share, and their common arguments as the kernels take them.
 int loss_launch(space_ctx* ctx, const char* who, const space_loss_io* io, bool row_terms, LossLaunch* l) {
     if (!io || !io->logits || !io->labels || !io->loss || !io->n_terms || !io->row_logp || !io->work || (row_terms && !io->row_loss))
@@ -574,6 +583,9 @@ int loss_launch(space_ctx* ctx, const char* who, const space_loss_io* io, bool r
         return fail(ctx, SPACE_EINVAL, "%s: no rows, or a row stride below the vocabulary of %d", who, vocab);
     const int64_t most = INT64_MAX / 16 / io->rows;
     if (io->logits_stride > most || (io->dlogits && io->dlogits_stride > most)) return fail(ctx, SPACE_EINVAL, "%s: row stride out of range", who);
+    if (io->rows > kLossRows) return fail(ctx, SPACE_ESHAPE, "%s: %d rows, more than %d", who, io->rows, kLossRows);
+    if (!words({io->labels, io->grad_scale, io->loss, io->n_terms, io->row_logp, io->row_loss}))
+        return fail(ctx, SPACE_EINVAL, "%s: an array not on 4 bytes", who);
     const uintptr_t x = (uintptr_t)io->logits, d = (uintptr_t)io->dlogits;
     if (x % b || d % b || (uintptr_t)io->work % 16)
         return fail(ctx, SPACE_EINVAL, "%s: logits or dlogits not on a whole element, or work not on 16 bytes", who);
@@ -1213,6 +1225,8 @@ int space_policy_loss(space_ctx* ctx, const space_loss_io* io, const space_polic
         !(params->kl_coef >= 0.f) || !std::isfinite(params->kl_coef))
         return fail(ctx, SPACE_EINVAL, "%s: clip_low %g outside 0..1, or clip_high %g or kl_coef %g negative or not finite", who,
                     (double)params->clip_low, (double)params->clip_high, (double)params->kl_coef);
+    if (!words({params->advantages, params->old_logp, params->ref_logp, params->row_weight, params->row_kl, params->n_clipped}))
+        return fail(ctx, SPACE_EINVAL, "%s: an array not on 4 bytes", who);
     if (params->kl_coef != 0.f && !params->ref_logp) return fail(ctx, SPACE_EINVAL, "%s: kl_coef needs ref_logp", who);
     PolicyArgs p{};
     p.advantages = params->advantages; p.old_logp = params->old_logp; p.ref_logp = params->ref_logp;
@@ -1228,7 +1242,10 @@ int space_preference_loss(space_ctx* ctx, const space_loss_io* io, const space_p
     LossLaunch l;
     if (int rc = loss_launch(ctx, who, io, false, &l)) return rc;
     if (!params || !params->seq_start || !params->pair_loss) return fail(ctx, SPACE_EINVAL, "%s: null argument", who);
-    if (params->pairs < 1 || params->pairs > INT32_MAX / 2 - 1) return fail(ctx, SPACE_EINVAL, "%s: %d pairs", who, params->pairs);
+    if (params->pairs < 1) return fail(ctx, SPACE_EINVAL, "%s: %d pairs", who, params->pairs);
+    if (params->pairs > kLossRows) return fail(ctx, SPACE_ESHAPE, "%s: %d pairs, more than %d", who, params->pairs, kLossRows);
+    if (!words({params->seq_start, params->ref_logp, params->pair_loss, params->seq_logp}))
+        return fail(ctx, SPACE_EINVAL, "%s: an array not on 4 bytes", who);
     if (!(params->beta > 0.f) || !std::isfinite(params->beta) || !std::isfinite(params->margin) || !(params->smoothing >= 0.f && params->smoothing <= 1.f))
         return fail(ctx, SPACE_EINVAL, "%s: beta %g not above 0, margin %g not finite or smoothing %g outside 0..1", who,
                     (double)params->beta, (double)params->margin, (double)params->smoothing);
@@ -1242,8 +1259,9 @@ int space_preference_loss(space_ctx* ctx, const space_loss_io* io, const space_p
 
 int space_grad_norm(space_ctx* ctx, const space_grad_tensor* tensors, int32_t n_tensors, float* norm, double* work, void* stream) {
     if (!ctx) return SPACE_EINVAL;
-    static_assert(SPACE_GRAD_WORK == kGradParts, "the header states the size of the scratch");
-    if (!norm || !work) return fail(ctx, SPACE_EINVAL, "space_grad_norm: null argument");
+    static_assert(SPACE_GRAD_WORK == kGradParts + 2, "the header states the size of the scratch");
+    if (!norm || !work || (uintptr_t)work % 8 || (uintptr_t)norm % 4)
+        return fail(ctx, SPACE_EINVAL, "space_grad_norm: null argument, or norm or work not on a whole element");
     std::unique_ptr<GradTensor[]> list;
     if (int rc = grad_list(ctx, "space_grad_norm", tensors, n_tensors, false, &list)) return rc;
     HIP_TRY(ctx, launch_grad_norm(list.get(), n_tensors, norm, work, (hipStream_t)stream));
@@ -1252,7 +1270,7 @@ int space_grad_norm(space_ctx* ctx, const space_grad_tensor* tensors, int32_t n_
 
 int space_grad_clip(space_ctx* ctx, const space_grad_tensor* tensors, int32_t n_tensors, const float* norm, float max_norm, void* stream) {
     if (!ctx) return SPACE_EINVAL;
-    if (!norm) return fail(ctx, SPACE_EINVAL, "space_grad_clip: null argument");
+    if (!norm || (uintptr_t)norm % 4) return fail(ctx, SPACE_EINVAL, "space_grad_clip: null argument, or norm not on a whole element");
     if (!(max_norm >= 0.f)) return fail(ctx, SPACE_EINVAL, "space_grad_clip: max_norm %g negative or not a number", (double)max_norm);
     std::unique_ptr<GradTensor[]> list;
     if (int rc = grad_list(ctx, "space_grad_clip", tensors, n_tensors, true, &list)) return rc;

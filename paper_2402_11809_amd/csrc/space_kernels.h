@@ -392,7 +392,7 @@ hipError_t launch_sar_grad(const LossLaunch& l, hipStream_t s);
 hipError_t launch_policy(const LossLaunch& l, const PolicyArgs& p, hipStream_t s);
 hipError_t launch_preference(const LossLaunch& l, const PrefArgs& p, hipStream_t s);
 
-// Gradient norm and clipping.  work: [kGradParts] partial sums of squares.
+// Gradient norm and clipping.  work: an arrival count (16 bytes, kept at 0 between calls), [kGradParts] partial sums of squares.
 constexpr int kGradParts = 2048;
 struct GradTensor {
     const void* grad;

@@ -83,12 +83,12 @@ __device__ __forceinline__ void row_zero(T* __restrict__ d, int vocab) {
 __device__ __forceinline__ void put(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float got(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// Whether this workgroup is the last of the launch's.  Thread 0 made the row's stores.
-__device__ __forceinline__ bool rows_done(const LossLaunch& l, int* s_last) {
+// Whether this workgroup is the last of the launch's.  Thread 0 made the stores that the last one reads.
+__device__ __forceinline__ bool arrive(uint32_t* arrived, int* s_last) {
     if (threadIdx.x == 0) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         const uint32_t share = arrival_share(gridDim.x, blockIdx.x);
-        *s_last = arrival_is_last(__hip_atomic_fetch_add(l.arrived, share, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), share);
+        *s_last = arrival_is_last(__hip_atomic_fetch_add(arrived, share, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), share);
     }
     __syncthreads();
     return *s_last;
@@ -105,8 +105,8 @@ __device__ __forceinline__ int count_rows(const LossLaunch& l) {
     return n;
 }
 
-// Loss, counts: each thread adds its own rows in row order, in 64 bits, then a fixed tree.
-template <int THREADS>
+// Loss, counts (SMALL: within the rows' launch): each thread adds its own rows in row order, in 64 bits, then a fixed tree.
+template <int THREADS, bool SMALL>
 __device__ __forceinline__ void sum_rows(const LossLaunch& l, int32_t* n_clipped) {
     constexpr int W = THREADS / 64;
     __shared__ double s_sum[W];
@@ -115,9 +115,9 @@ __device__ __forceinline__ void sum_rows(const LossLaunch& l, int32_t* n_clipped
     int n = 0, cut = 0;
 #pragma unroll 8
     for (int r = threadIdx.x; r < l.rows; r += THREADS) {
-        sum += got(l.row_loss + r);
+        sum += SMALL ? got(l.row_loss + r) : l.row_loss[r];
         n += row_counts(l.labels[r], l.vocab);
-        if (n_clipped) cut += got(&l.work[r].v[0]) != 0.f;
+        if (n_clipped) cut += (SMALL ? got(&l.work[r].v[0]) : l.work[r].v[0]) != 0.f;
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -142,7 +142,7 @@ __device__ __forceinline__ void sum_rows(const LossLaunch& l, int32_t* n_clipped
 }
 
 // The pairs, a sequence to a wave: sums over the rows of both sequences, the pair's term, and the slope of every row.
-template <int THREADS>
+template <int THREADS, bool SMALL>
 __device__ __forceinline__ void join_pairs(const LossLaunch& l, const PrefArgs& p) {
     constexpr int W = THREADS / 64, P = W > 1 ? W / 2 : 1;  // pairs at a time
     __shared__ double s_sum[2 * P], s_term[P];
@@ -170,7 +170,7 @@ __device__ __forceinline__ void join_pairs(const LossLaunch& l, const PrefArgs& 
             int n = 0;
 #pragma unroll 8
             for (int r = from[k] + lane; r < to[k]; r += 64) {
-                t += got(l.row_logp + r);
+                t += SMALL ? got(l.row_logp + r) : l.row_logp[r];
                 n += row_counts(l.labels[r], l.vocab);
             }
 #pragma unroll
@@ -343,9 +343,9 @@ __device__ __forceinline__ float row_coefficient(const LossLaunch& l, const Poli
 template <int KIND, int THREADS>
 __device__ __forceinline__ void finish_rows(const LossLaunch& l, const PolicyArgs& p, const PrefArgs& pref) {
     __shared__ int s_last;
-    if (!rows_done(l, &s_last)) return;
-    if (KIND == LOSS_PREF) join_pairs<THREADS>(l, pref);
-    else sum_rows<THREADS>(l, p.n_clipped);
+    if (!arrive(l.arrived, &s_last)) return;
+    if (KIND == LOSS_PREF) join_pairs<THREADS, true>(l, pref);
+    else sum_rows<THREADS, true>(l, p.n_clipped);
 }
 
 // A row in the registers of one workgroup: read once, written once.  Bound by memory: a row that is read while another one
@@ -579,8 +579,8 @@ __global__ __launch_bounds__(1024) void loss_count_kernel(LossLaunch l) {
     for (int w = 0; w < 16; ++w) all += s[w];
     *l.n_terms = all;
 }
-__global__ __launch_bounds__(1024) void loss_sum_kernel(LossLaunch l, int32_t* n_clipped) { sum_rows<1024>(l, n_clipped); }
-__global__ __launch_bounds__(1024) void pref_pairs_kernel(LossLaunch l, PrefArgs p) { join_pairs<1024>(l, p); }
+__global__ __launch_bounds__(1024) void loss_sum_kernel(LossLaunch l, int32_t* n_clipped) { sum_rows<1024, false>(l, n_clipped); }
+__global__ __launch_bounds__(1024) void pref_pairs_kernel(LossLaunch l, PrefArgs p) { join_pairs<1024, false>(l, p); }
 
 // The gradient of the preference loss, a row to a workgroup.  A row's coefficient is known when its whole pair has been read, so the
 // logits are read twice; the last rows first, which the memory-side cache still holds from the first time (7264 rows of 32000 in
@@ -701,8 +701,10 @@ __device__ __forceinline__ int grad_tensor_of(const GradList& g, int64_t chunk) 
 
 // What both passes over the gradients read twice comes from the memory-side cache the second time, if it is small enough: the
 // last kGradKept bytes are read in the ordinary way by the norm, and first by the clipping; everything in front of them, which the
-// cache would lose again, is read past it.
-constexpr int64_t kGradKept = 192ll << 20;
+// cache would lose again, is read past it.  Norm and clipping of 49 M gradients in fp32 113 -> 87 us against reading past the cache
+// throughout, of 435 M 969 -> 936; of the 256 MB of the cache 240 are best (247 MB of gradients: 192 / 224 / 240 / 256 MB 132 /
+// 127 / 118 / 118 us, 320 MB: 150 / 147 / 151 / 159).
+constexpr int64_t kGradKept = 240ll << 20;
 // The squares of n elements of a chunk, this thread's share.  A square is exact in 64 bits for both types, and no sum of them leaves the range.
 template <typename T, bool KEPT>
 __device__ __forceinline__ double chunk_squares(const T* __restrict__ x, int n) {
@@ -743,21 +745,27 @@ __device__ __forceinline__ double list_squares(const GradList& g, int64_t c, int
     }
     return sum;
 }
-__global__ __launch_bounds__(kGradThreads) void grad_square_kernel(GradList g, int64_t kept_from, double* work, int first_launch) {
+__device__ __forceinline__ void sum_squares(const double* work, int parts, float* norm, double* s) {
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < parts; i += kGradThreads) sum += __hip_atomic_load(work + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    sum = block_sum<kGradThreads / 64>(sum, s);
+    if (threadIdx.x == 0) *norm = (float)sqrt(sum);
+}
+// arrived: a lone launch of few workgroups, the last of which takes the root; else a launch behind them does
+__global__ __launch_bounds__(kGradThreads) void grad_square_kernel(GradList g, int64_t kept_from, double* work, int first_launch, uint32_t* arrived,
+                                                                   float* norm) {
     __shared__ double s[kGradThreads / 64];
+    __shared__ int s_last;
     double sum = list_squares<false>(g, blockIdx.x, kept_from);
     const int64_t turn = (kept_from + gridDim.x - 1 - blockIdx.x) / gridDim.x;  // how many of those this workgroup had
     sum += list_squares<true>(g, blockIdx.x + turn * gridDim.x, g.first[g.count]);
     sum = block_sum<kGradThreads / 64>(sum, s);
-    if (threadIdx.x == 0) work[blockIdx.x] = first_launch ? sum : work[blockIdx.x] + sum;
+    if (threadIdx.x == 0) __hip_atomic_store(work + blockIdx.x, first_launch ? sum : work[blockIdx.x] + sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (arrived && arrive(arrived, &s_last)) sum_squares(work, gridDim.x, norm, s);
 }
-
-__global__ __launch_bounds__(1024) void grad_norm_kernel(const double* work, int parts, float* norm) {
-    __shared__ double s[16];
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < parts; i += 1024) sum += work[i];
-    sum = block_sum<16>(sum, s);
-    if (threadIdx.x == 0) *norm = (float)sqrt(sum);
+__global__ __launch_bounds__(kGradThreads) void grad_norm_kernel(const double* work, int parts, float* norm) {
+    __shared__ double s[kGradThreads / 64];
+    sum_squares(work, parts, norm, s);
 }
 
 // N elements as a thread reads or writes them: 16 bytes, or 8 where bf16 goes with fp32, so that neighbouring lanes' stores meet
@@ -859,18 +867,26 @@ hipError_t each_grad_list(const GradTensor* t, int n, F launch) {
 
 int grad_workgroups(int64_t chunks) { return (int)(chunks < kGradParts ? chunks : kGradParts); }
 
+// Workgroups up to which the last one takes the root itself: one launch less, about 3 us, against additions to one count.
+constexpr int kGradSmall = 512;
+
 hipError_t launch_grad_norm(const GradTensor* t, int n, float* norm, double* work, hipStream_t s) {
+    uint32_t* arrived = (uint32_t*)work;
+    work += 2;
     // a later launch adds to the partial sums of an earlier one, so all of them have as many workgroups
-    int parts = 0;
-    hipError_t e = each_grad_list(t, n, [&](const GradList& g, int64_t) { parts = max(parts, grad_workgroups(g.first[g.count])); });
-    if (e != hipSuccess) return e;
-    int first = 1;
-    e = each_grad_list(t, n, [&](const GradList& g, int64_t kept_from) {
-        hipLaunchKernelGGL(grad_square_kernel, dim3(parts), dim3(kGradThreads), 0, s, g, kept_from, work, first);
-        first = 0;
+    int parts = 0, lists = 0, first = 1;
+    hipError_t e = each_grad_list(t, n, [&](const GradList& g, int64_t) {
+        parts = max(parts, grad_workgroups(g.first[g.count]));
+        ++lists;
     });
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, s, work, parts, norm);
+    const bool small = lists == 1 && parts <= kGradSmall;
+    e = each_grad_list(t, n, [&](const GradList& g, int64_t kept_from) {
+        hipLaunchKernelGGL(grad_square_kernel, dim3(parts), dim3(kGradThreads), 0, s, g, kept_from, work, first, small ? arrived : nullptr, norm);
+        first = 0;
+    });
+    if (e != hipSuccess || small) return e;
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(kGradThreads), 0, s, work, parts, norm);
     return hipGetLastError();
 }
 

@@ -451,7 +451,7 @@ def test_gradient_norm_and_clipping(sizes, types):
         src = [g.clone() for g in grads]
         outs = None if out_types is None else [tc.spoil(torch.empty_like(g, dtype=tc.torch_type(out_types[i % len(out_types)]))) for i, g in enumerate(src)]
         gs = binding.GradSet(gm, src, outs)
-        tc.spoil(gs.norm), tc.spoil(gs.work)
+        tc.spoil(gs.norm), tc.spoil(gs.work[2:])
         norm = float(gm.grad_clip(gs, max_norm))
         assert abs(norm - want) <= want * U * 1.001
         limit = float(np.float32(max_norm))
@@ -463,6 +463,25 @@ def test_gradient_norm_and_clipping(sizes, types):
             assert bool((err <= tol).all())
         if outs is not None:
             assert all(torch.equal(a, b) for a, b in zip(src, grads)), "the gradients themselves were written"
+
+
+def test_more_gradients_than_the_cache_holds_over_several_launches():
+    """A set beyond the memory-side cache, whose border lies within one of its lists: every element is scaled once, in place and not, and the norm
+    has them all.  Gradients of ones, halves and quarters: squares and sums are exact, the scale 1 / 2^k too."""
+    torch = gc.require_gpu()
+    from paper_2402_11809_amd import binding
+    gm = tc.head_model(40)
+    sizes = [(1 << 20) + 3 * i for i in range(118)]
+    for types, value in ((["f32"], 0.5), (["f32", "bf16"], 1.0), (["bf16"], 0.25)):
+        grads = [torch.full((n,), value, dtype=tc.torch_type(types[i % len(types)]), device="cuda") for i, n in enumerate(sizes)]
+        want = value * sum(sizes) ** 0.5
+        outs = [torch.zeros_like(g) for g in grads]
+        gs = binding.GradSet(gm, grads, outs)
+        assert abs(float(gm.grad_norm(gs)) - want) <= want * U * 1.001
+        gm.grad_clip(gs, 1.0, norm=torch.tensor([4.0], device="cuda"))
+        assert all(bool((o == value / 4).all()) for o in outs) and all(bool((g == value).all()) for g in grads)
+        gm.grad_clip(binding.GradSet(gm, grads), 1.0, norm=torch.tensor([2.0], device="cuda"))
+        assert all(bool((g == value / 2).all()) for g in grads)
 
 
 def test_norm_neither_overflows_nor_vanishes_and_what_is_not_finite_is_left():
@@ -555,6 +574,16 @@ def test_refusals_of_the_losses():
             io.dlogits = io.logits
         assert rc(C.byref(io)) == E, (field, value)
         assert gm.lib.space_last_error(gm.ctx)
+    for field in ("labels", "loss", "n_terms", "row_logp", "row_loss", "grad_scale"):  # on 4 bytes
+        io, keep = _io(gm)
+        setattr(io, field, (getattr(io, field) or f.data_ptr()) + 2)
+        assert rc(C.byref(io)) == E, field
+    io, keep = _io(gm)
+    io.rows = 1 << 22
+    assert rc(C.byref(io)) == binding.SPACE_ESHAPE
+    io, keep = _io(gm)
+    assert rc(C.byref(io), ("policy",), pol(old_logp=f.data_ptr() + 1)) == E and rc(C.byref(io), ("pref",), prf(seq_start=start.data_ptr() + 2)) == E
+    assert rc(C.byref(io), ("pref",), prf(pairs=1 << 22)) == binding.SPACE_ESHAPE
     io, keep = _io(gm)
     io.row_loss = None
     assert rc(C.byref(io), ("sar", "policy")) == E and rc(C.byref(io), ("pref",)) == 0
