@@ -141,84 +141,95 @@ __device__ __forceinline__ void sum_rows(const LossLaunch& l, int32_t* n_clipped
     if (n_clipped) *n_clipped = cut;
 }
 
-// The pairs, a sequence to a wave: sums over the rows of both sequences, the pair's term, and the slope of every row.
-template <int THREADS, bool SMALL>
-__device__ __forceinline__ void join_pairs(const LossLaunch& l, const PrefArgs& p) {
-    constexpr int W = THREADS / 64, P = W > 1 ? W / 2 : 1;  // pairs at a time
-    __shared__ double s_sum[2 * P], s_term[P];
-    __shared__ int s_n[2 * P];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    double all = 0.0;
-    int n_all = 0;
-    if (l.dlogits) {  // rows of no sequence
-        for (int r = threadIdx.x; r < l.rows; r += THREADS) l.work[r].v[3] = 0.f;
-        __syncthreads();
-    }
-    for (int first = 0; first < p.pairs; first += P) {
-        int from[2] = {}, to[2] = {};
-        // (a lone wave has both sequences of a pair in turn)
-        const int turns = W > 1 ? 1 : 2;
-#pragma unroll
-        for (int k = 0; k < turns; ++k) {
-            const int at = W > 1 ? wave : k, seq = 2 * first + at;
-            if (seq >= 2 * p.pairs) break;
-            const int a = p.seq_start[seq], b = p.seq_start[seq + 1];
-            from[k] = min(max(a, 0), l.rows);
-            to[k] = min(max(b, from[k]), l.rows);
-            if (lane == 0 && (a != from[k] || b != to[k])) atomicAdd(l.faults, 1);
-            double t = 0.0;
-            int n = 0;
+// ---- the preference loss
+// Sequence `seq` by one wave: its rows (clamped to those there are), how many count, and their sum or mean of logp.
+struct SeqSum {
+    int from, to, n;
+    double sum;
+    bool fault;
+};
+__device__ __forceinline__ SeqSum sum_sequence(const LossLaunch& l, const PrefArgs& p, int seq) {
+    SeqSum q;
+    const int a = p.seq_start[seq], b = p.seq_start[seq + 1];
+    q.from = min(max(a, 0), l.rows);
+    q.to = min(max(b, q.from), l.rows);
+    q.fault = a != q.from || b != q.to;
+    q.sum = 0.0;
+    q.n = 0;
 #pragma unroll 8
-            for (int r = from[k] + lane; r < to[k]; r += 64) {
-                t += SMALL ? got(l.row_logp + r) : l.row_logp[r];
-                n += row_counts(l.labels[r], l.vocab);
-            }
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) {
-                t += __shfl_xor(t, o, 64);
-                n += __shfl_xor(n, o, 64);
-            }
-            if (p.average) t /= max(n, 1);
-            if (lane == 0) {
-                s_sum[at] = p.ref_logp ? t - p.ref_logp[seq] : t;
-                s_n[at] = n;
-                if (p.seq_logp) p.seq_logp[seq] = (float)t;
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < turns; ++k) {
-            const int at = W > 1 ? wave : k, pair = first + at / 2;
-            if (pair >= p.pairs) break;
-            const double z = (double)p.beta * (s_sum[at & ~1] - s_sum[at | 1]) - (double)p.margin, eps = p.smoothing;
-            const double far = exp(-fabs(z)), tail = log1p(far);
-            if (lane == 0 && at % 2 == 0) {
-                const double low = fmax(-z, 0.0) + tail, high = fmax(z, 0.0) + tail;  // softplus(-z), softplus(z)
-                const double term = (eps < 1.0 ? (1.0 - eps) * low : 0.0) + (eps > 0.0 ? eps * high : 0.0);
-                p.pair_loss[pair] = (float)term;
-                s_term[at / 2] = term;
-            }
-            if (!l.dlogits) continue;
-            // sigmoid(z) and sigmoid(-z), each without a difference from 1
-            const double big = 1.0 / (1.0 + far), small = far / (1.0 + far);
-            double c = (double)p.beta * (eps * (z >= 0.0 ? big : small) - (1.0 - eps) * (z >= 0.0 ? small : big));
-            if (l.mean) c /= p.pairs;
-            if (l.grad_scale) c *= *l.grad_scale;
-            if (p.average) c /= max(s_n[at], 1);
-            const float slope = (float)(at % 2 ? -c : c);
-            for (int r = from[k] + lane; r < to[k]; r += 64) l.work[r].v[3] = slope;
-        }
-        __syncthreads();
-        if (threadIdx.x == 0)
-            for (int k = 0; k < P && first + k < p.pairs; ++k) {
-                all += s_term[k];
-                n_all += s_n[2 * k] + s_n[2 * k + 1];
-            }
-        __syncthreads();
+    for (int r = q.from + (threadIdx.x & 63); r < q.to; r += 64) {
+        q.sum += l.row_logp[r];
+        q.n += row_counts(l.labels[r], l.vocab);
     }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        q.sum += __shfl_xor(q.sum, o, 64);
+        q.n += __shfl_xor(q.n, o, 64);
+    }
+    if (p.average) q.sum /= max(q.n, 1);
+    return q;
+}
+__device__ __forceinline__ double against_reference(const PrefArgs& p, int seq, double sum) { return p.ref_logp ? sum - p.ref_logp[seq] : sum; }
+
+struct PairTerm {
+    double term, slope;  // slope: along z, times the caller's factors
+};
+__device__ __forceinline__ PairTerm pair_term(const LossLaunch& l, const PrefArgs& p, double chosen, double rejected) {
+    const double z = (double)p.beta * (chosen - rejected) - (double)p.margin, eps = p.smoothing;
+    const double far = exp(-fabs(z)), tail = log1p(far);
+    const double low = fmax(-z, 0.0) + tail, high = fmax(z, 0.0) + tail;  // softplus(-z), softplus(z)
+    PairTerm t;
+    t.term = (eps < 1.0 ? (1.0 - eps) * low : 0.0) + (eps > 0.0 ? eps * high : 0.0);
+    // sigmoid(z) and sigmoid(-z), each without a difference from 1
+    const double big = 1.0 / (1.0 + far), small = far / (1.0 + far);
+    t.slope = (double)p.beta * (eps * (z >= 0.0 ? big : small) - (1.0 - eps) * (z >= 0.0 ? small : big));
+    if (l.mean) t.slope /= p.pairs;
+    if (l.grad_scale) t.slope *= *l.grad_scale;
+    return t;
+}
+// Of a row of the chosen (which = 0) or the rejected sequence, in which n rows count
+__device__ __forceinline__ float row_slope_of(const PrefArgs& p, const PairTerm& t, int which, int n) {
+    const double c = p.average ? t.slope / max(n, 1) : t.slope;
+    return (float)(which ? -c : c);
+}
+
+// Eight pairs to a workgroup of 1024 threads, a sequence to a wave: the pairs' terms and, where WRITE, the slopes of the rows.
+constexpr int kPairs = 8;
+template <bool WRITE>
+__device__ __forceinline__ void join_pairs(const LossLaunch& l, const PrefArgs& p, int first) {
+    __shared__ double s_sum[2 * kPairs];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, seq = 2 * first + wave;
+    SeqSum q;
+    if (seq < 2 * p.pairs) {
+        q = sum_sequence(l, p, seq);
+        if (lane == 0) {
+            s_sum[wave] = against_reference(p, seq, q.sum);
+            if (p.seq_logp) p.seq_logp[seq] = (float)q.sum;
+            if (q.fault) atomicAdd(l.faults, 1);
+        }
+    }
+    __syncthreads();
+    if (seq >= 2 * p.pairs) return;
+    const PairTerm t = pair_term(l, p, s_sum[wave & ~1], s_sum[wave | 1]);
+    if (lane == 0 && wave % 2 == 0) p.pair_loss[seq / 2] = (float)t.term;
+    if (!WRITE) return;
+    const float slope = row_slope_of(p, t, wave % 2, q.n);
+    for (int r = q.from + lane; r < q.to; r += 64) l.work[r].v[3] = slope;
+}
+
+// The loss, from the pairs' terms, and the rows that count: 1024 threads, a fixed order, 64 bits.
+__device__ __forceinline__ void sum_pairs(const LossLaunch& l, const PrefArgs& p) {
+    __shared__ double s[16];
+    double sum = 0.0, n = 0.0;
+    for (int i = threadIdx.x; i < p.pairs; i += 1024) sum += p.pair_loss[i];
+    const int from = min(max(p.seq_start[0], 0), l.rows), to = min(max(p.seq_start[2 * p.pairs], 0), l.rows);
+#pragma unroll 4
+    for (int r = from + threadIdx.x; r < to; r += 1024) n += row_counts(l.labels[r], l.vocab);
+    sum = block_sum<16>(sum, s);
+    n = block_sum<16>(n, s);
     if (threadIdx.x == 0) {
-        *l.loss = (float)(l.mean ? all / p.pairs : all);
-        *l.n_terms = n_all;
+        *l.loss = (float)(l.mean ? sum / p.pairs : sum);
+        *l.n_terms = (int)n;
     }
 }
 
@@ -340,12 +351,10 @@ __device__ __forceinline__ float row_coefficient(const LossLaunch& l, const Poli
 }
 
 // Behind a row: the last workgroup adds up.
-template <int KIND, int THREADS>
-__device__ __forceinline__ void finish_rows(const LossLaunch& l, const PolicyArgs& p, const PrefArgs& pref) {
+template <int THREADS>
+__device__ __forceinline__ void finish_rows(const LossLaunch& l, const PolicyArgs& p) {
     __shared__ int s_last;
-    if (!arrive(l.arrived, &s_last)) return;
-    if (KIND == LOSS_PREF) join_pairs<THREADS, true>(l, pref);
-    else sum_rows<THREADS, true>(l, p.n_clipped);
+    if (arrive(l.arrived, &s_last)) sum_rows<THREADS, true>(l, p.n_clipped);
 }
 
 // A row in the registers of one workgroup: read once, written once.  Bound by memory: a row that is read while another one
@@ -456,9 +465,9 @@ __device__ __forceinline__ void row_of_loss(const LossLaunch& l, const PolicyArg
 }
 
 template <typename T, int KIND, int THREADS, int NV, bool KEEP, bool SMALL>
-__global__ __launch_bounds__(THREADS, 4) void loss_rows_kernel(LossLaunch l, PolicyArgs p, PrefArgs pref) {
+__global__ __launch_bounds__(THREADS, 4) void loss_rows_kernel(LossLaunch l, PolicyArgs p) {
     row_of_loss<T, KIND, THREADS, NV, KEEP, SMALL>(l, p);
-    if (SMALL) finish_rows<KIND, THREADS>(l, p, pref);
+    if (SMALL) finish_rows<THREADS>(l, p);
 }
 
 // A row that no workgroup's registers hold: once for maximum and sum, once for the gradient.
@@ -563,9 +572,9 @@ __device__ __forceinline__ void long_row_of_loss(const LossLaunch& l, const Poli
 }
 
 template <typename T, int KIND, bool SMALL>
-__global__ __launch_bounds__(kLongThreads) void loss_long_rows_kernel(LossLaunch l, PolicyArgs p, PrefArgs pref) {
+__global__ __launch_bounds__(kLongThreads) void loss_long_rows_kernel(LossLaunch l, PolicyArgs p) {
     long_row_of_loss<T, KIND, SMALL>(l, p);
-    if (SMALL) finish_rows<KIND, kLongThreads>(l, p, pref);
+    if (SMALL) finish_rows<kLongThreads>(l, p);
 }
 
 // How many rows count, for the mean that the rows' gradients need before the rows are done.
@@ -580,18 +589,67 @@ __global__ __launch_bounds__(1024) void loss_count_kernel(LossLaunch l) {
     *l.n_terms = all;
 }
 __global__ __launch_bounds__(1024) void loss_sum_kernel(LossLaunch l, int32_t* n_clipped) { sum_rows<1024, false>(l, n_clipped); }
-__global__ __launch_bounds__(1024) void pref_pairs_kernel(LossLaunch l, PrefArgs p) { join_pairs<1024, false>(l, p); }
+__global__ __launch_bounds__(1024) void pref_pairs_kernel(LossLaunch l, PrefArgs p) {
+    if (l.dlogits) {  // rows of no sequence
+        const int from = p.seq_start[0], to = p.seq_start[2 * p.pairs];
+        for (int r = blockIdx.x * 1024 + threadIdx.x; r < l.rows; r += gridDim.x * 1024)
+            if (r < from || r >= to) l.work[r].v[3] = 0.f;
+        join_pairs<true>(l, p, blockIdx.x * kPairs);
+    } else {
+        join_pairs<false>(l, p, blockIdx.x * kPairs);
+    }
+    if (gridDim.x > 1) return;
+    __syncthreads();
+    sum_pairs(l, p);
+}
+__global__ __launch_bounds__(1024) void pref_sum_kernel(LossLaunch l, PrefArgs p) { sum_pairs(l, p); }
 
 // The gradient of the preference loss, a row to a workgroup.  A row's coefficient is known when its whole pair has been read, so the
 // logits are read twice; the last rows first, which the memory-side cache still holds from the first time (7264 rows of 32000 in
 // bf16, six in ten counting: both passes 197 -> 171 us).
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS) void pref_gradient_kernel(LossLaunch l) {
-    const int row = l.rows - 1 - blockIdx.x, label = l.labels[row];
+__device__ __forceinline__ void pref_row(const LossLaunch& l, int row, int label, float slope) {
     T* d = (T*)l.dlogits + (size_t)row * l.dlogits_stride;
+    if (!row_counts(label, l.vocab) || slope == 0.f) return row_zero<T, THREADS>(d, l.vocab);
     const f32x4_raw f = l.work[row];
-    if (!row_counts(label, l.vocab) || f.v[3] == 0.f) return row_zero<T, THREADS>(d, l.vocab);
-    long_gradient<T, THREADS>((const T*)l.logits + (size_t)row * l.logits_stride, d, l.vocab, label, f.v[0], -f.v[3] * f.v[1], f.v[3] * f.v[2]);
+    long_gradient<T, THREADS>((const T*)l.logits + (size_t)row * l.logits_stride, d, l.vocab, label, f.v[0], -slope * f.v[1], slope * f.v[2]);
+}
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void pref_gradient_kernel(LossLaunch l) {
+    const int row = l.rows - 1 - blockIdx.x;
+    pref_row<T, THREADS>(l, row, l.labels[row], l.work[row].v[3]);
+}
+// A call of up to kPairs pairs and kPrefSmall rows does without a launch for the pairs: every row's workgroup adds up the two sequences
+// itself, a wave each, and one workgroup more writes what the pairs give out (43 rows of 32000 in bf16 13.8 -> 12.6 us; from a
+// workgroup per CU on it costs more than the launch: 803 rows of 5003 in fp32 16.7 -> 20.0).
+constexpr int kPrefSmall = 256;
+template <typename T>
+__global__ __launch_bounds__(1024) void pref_small_kernel(LossLaunch l, PrefArgs p) {
+    if (blockIdx.x == 0) {  // (first, as it takes longest)
+        join_pairs<false>(l, p, 0);
+        __syncthreads();
+        return sum_pairs(l, p);
+    }
+    __shared__ SeqSum s_seq[2];
+    __shared__ float s_slope;
+    const int row = l.rows - blockIdx.x, label = l.labels[row], wave = threadIdx.x >> 6;
+    int seq = -1;  // the row's sequence: how many begin at or in front of it
+    for (int i = 0; i <= 2 * p.pairs; ++i) seq += p.seq_start[i] <= row;
+    float slope = 0.f;
+    if (row_counts(label, l.vocab) && seq >= 0 && seq < 2 * p.pairs) {  // (all threads)
+        if (wave < 2) {
+            const SeqSum q = sum_sequence(l, p, (seq & ~1) + wave);
+            if ((threadIdx.x & 63) == 0) s_seq[wave] = q;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            const PairTerm t = pair_term(l, p, against_reference(p, seq & ~1, s_seq[0].sum), against_reference(p, seq | 1, s_seq[1].sum));
+            if (threadIdx.x == 0) s_slope = row_slope_of(p, t, seq & 1, s_seq[seq & 1].n);
+        }
+        __syncthreads();
+        slope = s_slope;
+    }
+    pref_row<T, 1024>(l, row, label, slope);
 }
 template <typename T>
 hipError_t launch_pref_gradient(const LossLaunch& l, hipStream_t s) {
@@ -603,11 +661,11 @@ hipError_t launch_pref_gradient(const LossLaunch& l, hipStream_t s) {
 }
 
 template <typename T, int KIND, bool SMALL>
-hipError_t launch_rows_of(const LossLaunch& l, const PolicyArgs& p, const PrefArgs& pref, hipStream_t s) {
+hipError_t launch_rows_of(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) {
     constexpr int E = Vec<T>::N;
     const dim3 grid(l.rows);
 #define SPACE_ROWS(THREADS, ELEMS, KEEP) \
-    hipLaunchKernelGGL((loss_rows_kernel<T, KIND, THREADS, (ELEMS) / E, KEEP, SMALL>), grid, dim3(THREADS), 0, s, l, p, pref)
+    hipLaunchKernelGGL((loss_rows_kernel<T, KIND, THREADS, (ELEMS) / E, KEEP, SMALL>), grid, dim3(THREADS), 0, s, l, p)
     if (l.vocab <= 64 * 32) {
         SPACE_ROWS(64, 32, true);
     } else if (l.vocab <= 128 * 32) {
@@ -633,29 +691,30 @@ hipError_t launch_rows_of(const LossLaunch& l, const PolicyArgs& p, const PrefAr
                 return hipGetLastError();
             }
         }
-        hipLaunchKernelGGL((loss_long_rows_kernel<T, KIND, SMALL>), grid, dim3(kLongThreads), 0, s, l, p, pref);
+        hipLaunchKernelGGL((loss_long_rows_kernel<T, KIND, SMALL>), grid, dim3(kLongThreads), 0, s, l, p);
     }
 #undef SPACE_ROWS
     return hipGetLastError();
 }
-template <int KIND>
-hipError_t launch_rows(const LossLaunch& l, const PolicyArgs& p, const PrefArgs& pref, bool small, hipStream_t s) {
-    if (l.dtype == 0) return small ? launch_rows_of<float, KIND, true>(l, p, pref, s) : launch_rows_of<float, KIND, false>(l, p, pref, s);
-    return small ? launch_rows_of<uint16_t, KIND, true>(l, p, pref, s) : launch_rows_of<uint16_t, KIND, false>(l, p, pref, s);
+template <int KIND, bool SMALL>
+hipError_t launch_rows(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) {
+    return l.dtype == 0 ? launch_rows_of<float, KIND, SMALL>(l, p, s) : launch_rows_of<uint16_t, KIND, SMALL>(l, p, s);
 }
 
-// Whether the rows' workgroups count and add up themselves.  That saves two launches (about 6 us of 15), but every workgroup reads
-// all labels and adds to one count.
-bool small_call(const LossLaunch& l) { return l.rows <= 2048 && (int64_t)l.rows * 4 <= (int64_t)l.vocab * (l.dtype ? 2 : 4) / 8; }
+// Whether the rows' workgroups count and add up themselves.  That saves two launches (one where nothing has to be counted first), 3 -
+// 4 us, but every workgroup reads all labels and adds to one count, which takes 13 ns each: no matter where a row takes longer
+// (4000 rows of 32000 in fp32 167 -> 163 us, 500 in bf16 17 -> 15; 8000 in bf16 level), and less than the launches up to about 200
+// short rows (200 rows of 1000 in fp32 9.0 -> 8.2 us, 500 of them 9.3 -> 11.0, 2000 11.8 -> 30).
+bool small_call(const LossLaunch& l) { return l.rows <= 192 || (l.rows <= 4096 && (int64_t)l.vocab * (l.dtype ? 2 : 4) >= 48 * 1024); }
 
 template <int KIND>
 hipError_t launch_loss(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) {
-    if (small_call(l)) return launch_rows<KIND>(l, p, PrefArgs{}, true, s);
+    if (small_call(l)) return launch_rows<KIND, true>(l, p, s);
     if (l.mean && l.dlogits) {
         hipLaunchKernelGGL(loss_count_kernel, dim3(1), dim3(1024), 0, s, l);
         if (hipError_t e = hipGetLastError()) return e;
     }
-    if (hipError_t e = launch_rows<KIND>(l, p, PrefArgs{}, false, s)) return e;
+    if (hipError_t e = launch_rows<KIND, false>(l, p, s)) return e;
     hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, s, l, p.n_clipped);
     return hipGetLastError();
 }
@@ -664,10 +723,18 @@ hipError_t launch_sar_grad(const LossLaunch& l, hipStream_t s) { return launch_l
 hipError_t launch_policy(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) { return launch_loss<LOSS_POLICY>(l, p, s); }
 
 hipError_t launch_preference(const LossLaunch& l, const PrefArgs& p, hipStream_t s) {
-    const bool small = small_call(l);
-    if (hipError_t e = launch_rows<LOSS_PREF>(l, PolicyArgs{}, p, small, s)) return e;
-    if (!small) {
-        hipLaunchKernelGGL(pref_pairs_kernel, dim3(1), dim3(1024), 0, s, l, p);
+    if (hipError_t e = launch_rows<LOSS_PREF, false>(l, PolicyArgs{}, s)) return e;
+    if (l.dlogits && l.rows <= kPrefSmall && p.pairs <= kPairs) {
+        const dim3 grid(l.rows + 1);
+        if (l.dtype == 0) hipLaunchKernelGGL(pref_small_kernel<float>, grid, dim3(1024), 0, s, l, p);
+        else hipLaunchKernelGGL(pref_small_kernel<uint16_t>, grid, dim3(1024), 0, s, l, p);
+        return hipGetLastError();
+    }
+    const int wgs = (p.pairs + kPairs - 1) / kPairs;
+    hipLaunchKernelGGL(pref_pairs_kernel, dim3(wgs), dim3(1024), 0, s, l, p);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (wgs > 1) {
+        hipLaunchKernelGGL(pref_sum_kernel, dim3(1), dim3(1024), 0, s, l, p);
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (!l.dlogits) return hipSuccess;

@@ -254,7 +254,10 @@ def test_ratios_that_overflow_or_vanish():
 
 PREF = [  # V, sequence lengths, rows in front, rows behind
     (1000, [1, 1], 0, 0), (1000, [0, 5], 0, 0), (1000, [0, 0, 3, 4], 2, 3), (32000, [24, 19], 0, 2),
-    (4099, [7, 130, 64, 1, 33, 65, 2, 0], 1, 0), (50, list(np.arange(66) % 9), 0, 5), (131079, [3, 2], 0, 0)]
+    (4099, [7, 130, 64, 1, 33, 65, 2, 0], 1, 0), (50, list(np.arange(66) % 9), 0, 5), (131079, [3, 2], 0, 0),
+    # on both sides of what one launch does for the pairs as well: rows, pairs; every width of the launch behind it
+    (1000, [130, 120], 3, 3), (1000, [130, 121], 3, 3), (1000, [700, 600], 0, 3), (300, [5] * 16, 0, 1), (300, [5] * 18, 0, 1), (4100, [600, 700], 1, 2), (20000, [530, 511], 0, 0),
+    (40, [0] * 40 + [3] * 100, 0, 0)]
 
 
 @pytest.mark.parametrize("average,smoothing,with_ref,mean", [(False, 0.0, True, True), (True, 0.2, False, False)])
