@@ -193,31 +193,51 @@ __device__ __forceinline__ float row_slope_of(const PrefArgs& p, const PairTerm&
     return (float)(which ? -c : c);
 }
 
-// Eight pairs to a workgroup of 1024 threads, a sequence to a wave: the pairs' terms and, where WRITE, the slopes of the rows.
+// Eight pairs to a workgroup of 1024 threads, a sequence to a wave: the pairs' terms and, where WRITE, the slopes of the rows.  A
+// workgroup that has all pairs adds them up, too.
 constexpr int kPairs = 8;
 template <bool WRITE>
 __device__ __forceinline__ void join_pairs(const LossLaunch& l, const PrefArgs& p, int first) {
-    __shared__ double s_sum[2 * kPairs];
+    __shared__ double s_sum[2 * kPairs], s_term[kPairs];
+    __shared__ int s_n[2 * kPairs];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, seq = 2 * first + wave;
+    const bool mine = seq < 2 * p.pairs;
     SeqSum q;
-    if (seq < 2 * p.pairs) {
+    if (mine) {
         q = sum_sequence(l, p, seq);
         if (lane == 0) {
             s_sum[wave] = against_reference(p, seq, q.sum);
+            s_n[wave] = q.n;
             if (p.seq_logp) p.seq_logp[seq] = (float)q.sum;
             if (q.fault) atomicAdd(l.faults, 1);
         }
     }
     __syncthreads();
-    if (seq >= 2 * p.pairs) return;
-    const PairTerm t = pair_term(l, p, s_sum[wave & ~1], s_sum[wave | 1]);
-    if (lane == 0 && wave % 2 == 0) p.pair_loss[seq / 2] = (float)t.term;
-    if (!WRITE) return;
-    const float slope = row_slope_of(p, t, wave % 2, q.n);
-    for (int r = q.from + lane; r < q.to; r += 64) l.work[r].v[3] = slope;
+    if (mine) {
+        const PairTerm t = pair_term(l, p, s_sum[wave & ~1], s_sum[wave | 1]);
+        if (lane == 0 && wave % 2 == 0) {
+            p.pair_loss[seq / 2] = (float)t.term;
+            s_term[wave / 2] = t.term;
+        }
+        if (WRITE) {
+            const float slope = row_slope_of(p, t, wave % 2, q.n);
+            for (int r = q.from + lane; r < q.to; r += 64) l.work[r].v[3] = slope;
+        }
+    }
+    if (p.pairs > kPairs) return;
+    __syncthreads();  // no others: the loss, too
+    if (threadIdx.x != 0) return;
+    double sum = 0.0;
+    int n = 0;
+    for (int k = 0; k < p.pairs; ++k) {
+        sum += s_term[k];
+        n += s_n[2 * k] + s_n[2 * k + 1];
+    }
+    *l.loss = (float)(l.mean ? sum / p.pairs : sum);
+    *l.n_terms = n;
 }
 
-// The loss, from the pairs' terms, and the rows that count: 1024 threads, a fixed order, 64 bits.
+// The loss of many pairs, from their terms, and the rows that count: 1024 threads, a fixed order, 64 bits.
 __device__ __forceinline__ void sum_pairs(const LossLaunch& l, const PrefArgs& p) {
     __shared__ double s[16];
     double sum = 0.0, n = 0.0;
@@ -289,7 +309,7 @@ __device__ __forceinline__ RowSlope row_slope(const PolicyArgs& p, int row, doub
         s.slope = s.clipped ? 0.0 : -u;
         if (p.ref_logp) {
             const double gap = p.ref_logp[row] - logp, em = expm1(gap);
-            s.kl = em - gap;
+            s.kl = em == INFINITY ? em : em - gap;  // (a token that is masked out now)
             if (p.kl_coef != 0.f) {
                 s.term += (double)p.kl_coef * s.kl;
                 s.slope -= (double)p.kl_coef * em;
@@ -598,9 +618,6 @@ __global__ __launch_bounds__(1024) void pref_pairs_kernel(LossLaunch l, PrefArgs
     } else {
         join_pairs<false>(l, p, blockIdx.x * kPairs);
     }
-    if (gridDim.x > 1) return;
-    __syncthreads();
-    sum_pairs(l, p);
 }
 __global__ __launch_bounds__(1024) void pref_sum_kernel(LossLaunch l, PrefArgs p) { sum_pairs(l, p); }
 
@@ -625,11 +642,7 @@ __global__ __launch_bounds__(THREADS) void pref_gradient_kernel(LossLaunch l) {
 constexpr int kPrefSmall = 256;
 template <typename T>
 __global__ __launch_bounds__(1024) void pref_small_kernel(LossLaunch l, PrefArgs p) {
-    if (blockIdx.x == 0) {  // (first, as it takes longest)
-        join_pairs<false>(l, p, 0);
-        __syncthreads();
-        return sum_pairs(l, p);
-    }
+    if (blockIdx.x == 0) return join_pairs<false>(l, p, 0);  // (first, as it takes longest)
     __shared__ SeqSum s_seq[2];
     __shared__ float s_slope;
     const int row = l.rows - blockIdx.x, label = l.labels[row], wave = threadIdx.x >> 6;
@@ -778,24 +791,23 @@ __device__ __forceinline__ double chunk_squares(const T* __restrict__ x, int n) 
     typedef Vec<T> V;
     constexpr int E = V::N, NV = kGradChunk / kGradThreads / E;
     double sum[2] = {0.0, 0.0};
-    const int tid = threadIdx.x;
-    if (n == kGradChunk) {
-        typename V::raw q[NV];
+    const int tid = threadIdx.x, whole = n / E, odd = whole * E + tid;
+    typename V::raw q[NV];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) q[j] = read_vec<KEPT, V>(x + (tid + j * kGradThreads) * E);
+    for (int j = 0; j < NV; ++j)
+        if (tid + j * kGradThreads < whole) q[j] = read_vec<KEPT, V>(x + (tid + j * kGradThreads) * E);
+    if (odd < n) {
+        const double v = load_f32(x + odd);
+        sum[0] = v * v;
+    }
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
+    for (int j = 0; j < NV; ++j)
+        if (tid + j * kGradThreads < whole) {
             float v[E];
             V::get(q[j], v);
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[e & 1] = fma((double)v[e], (double)v[e], sum[e & 1]);
         }
-    } else {
-        for (int i = tid; i < n; i += kGradThreads) {
-            const double v = load_f32(x + i);
-            sum[0] = fma(v, v, sum[0]);
-        }
-    }
     return sum[0] + sum[1];
 }
 
@@ -812,10 +824,11 @@ __device__ __forceinline__ double list_squares(const GradList& g, int64_t c, int
     }
     return sum;
 }
+template <int THREADS, bool SMALL>
 __device__ __forceinline__ void sum_squares(const double* work, int parts, float* norm, double* s) {
     double sum = 0.0;
-    for (int i = threadIdx.x; i < parts; i += kGradThreads) sum += __hip_atomic_load(work + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    sum = block_sum<kGradThreads / 64>(sum, s);
+    for (int i = threadIdx.x; i < parts; i += THREADS) sum += SMALL ? __hip_atomic_load(work + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : work[i];
+    sum = block_sum<THREADS / 64>(sum, s);
     if (threadIdx.x == 0) *norm = (float)sqrt(sum);
 }
 // arrived: a lone launch of few workgroups, the last of which takes the root; else a launch behind them does
@@ -828,11 +841,11 @@ __global__ __launch_bounds__(kGradThreads) void grad_square_kernel(GradList g, i
     sum += list_squares<true>(g, blockIdx.x + turn * gridDim.x, g.first[g.count]);
     sum = block_sum<kGradThreads / 64>(sum, s);
     if (threadIdx.x == 0) __hip_atomic_store(work + blockIdx.x, first_launch ? sum : work[blockIdx.x] + sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (arrived && arrive(arrived, &s_last)) sum_squares(work, gridDim.x, norm, s);
+    if (arrived && arrive(arrived, &s_last)) sum_squares<kGradThreads, true>(work, gridDim.x, norm, s);
 }
-__global__ __launch_bounds__(kGradThreads) void grad_norm_kernel(const double* work, int parts, float* norm) {
-    __shared__ double s[kGradThreads / 64];
-    sum_squares(work, parts, norm, s);
+__global__ __launch_bounds__(1024) void grad_norm_kernel(const double* work, int parts, float* norm) {
+    __shared__ double s[16];
+    sum_squares<1024, false>(work, parts, norm, s);
 }
 
 // N elements as a thread reads or writes them: 16 bytes, or 8 where bf16 goes with fp32, so that neighbouring lanes' stores meet
@@ -862,20 +875,19 @@ template <> struct Some<uint16_t, 4> {
 template <bool KEPT, typename T, typename O>
 __device__ __forceinline__ void chunk_scale(const T* x, O* y, int n, float scale) {
     constexpr int E = sizeof(T) == 2 && sizeof(O) == 2 ? 8 : 4, NV = kGradChunk / kGradThreads / E;
-    const int tid = threadIdx.x;
-    if (n == kGradChunk) {
-        float v[NV][E];
+    const int tid = threadIdx.x, whole = n / E, odd = whole * E + tid;
+    float v[NV][E];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) Some<T, E>::template load<KEPT>(x + (tid + j * kGradThreads) * E, v[j]);
+    for (int j = 0; j < NV; ++j)
+        if (tid + j * kGradThreads < whole) Some<T, E>::template load<KEPT>(x + (tid + j * kGradThreads) * E, v[j]);
+    if (odd < n) store_f32(y + odd, load_f32(x + odd) * scale);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
+    for (int j = 0; j < NV; ++j)
+        if (tid + j * kGradThreads < whole) {
 #pragma unroll
             for (int e = 0; e < E; ++e) v[j][e] *= scale;
             Some<O, E>::store(y + (tid + j * kGradThreads) * E, v[j]);
         }
-    } else {
-        for (int i = tid; i < n; i += kGradThreads) store_f32(y + i, load_f32(x + i) * scale);
-    }
 }
 
 template <bool KEPT>
@@ -953,7 +965,7 @@ hipError_t launch_grad_norm(const GradTensor* t, int n, float* norm, double* wor
         first = 0;
     });
     if (e != hipSuccess || small) return e;
-    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(kGradThreads), 0, s, work, parts, norm);
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, s, work, parts, norm);
     return hipGetLastError();
 }
 

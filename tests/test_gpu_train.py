@@ -252,6 +252,30 @@ def test_ratios_that_overflow_or_vanish():
     assert bool((out.dlogits[0] == 0).all()) and bool(torch.isfinite(out.dlogits).all())
 
 
+def test_policy_loss_of_tokens_that_one_of_the_models_masks():
+    """-inf as this model's, the old one's or the reference's log probability: limits of the formulas, not differences of infinities."""
+    torch = gc.require_gpu()
+    V, inf = 64, float("inf")
+    gm = tc.head_model(V)
+    x, _ = tc.make_logits(np.random.default_rng(4), 4, V, "f32")
+    labels = torch.full((4,), 9, dtype=torch.int32, device="cuda")
+    x[0, 9] = -inf                                                     # ratio 0, KL infinite
+    adv = torch.tensor([1.0, 1.0, 1.0, -1.0], device="cuda")
+    old = torch.tensor([-2.0, -inf, -2.0, -2.0], device="cuda")        # ratio infinite: clipped
+    ref = torch.tensor([-1.0, -1.0, -inf, -1.0], device="cuda")        # KL infinite, its slope the coefficient
+    out = tc.fresh_out(gm, 4, "f32")
+    gm.policy_loss(x, labels, adv, out, old_logp=old, ref_logp=ref, mean=False)
+    lp = tc.Rows64(x, labels).logp
+    assert float(out.row_logp[0]) == -inf and float(out.row_loss[0]) == 0.0 and bool((out.dlogits[0] == 0).all()) and float(out.row_kl[0]) == inf
+    assert float(out.row_loss[1]) == -float(np.float32(1) + np.float32(0.2)) and bool((out.dlogits[1] == 0).all()) and int(out.n_clipped) >= 1
+    assert float(out.row_kl[2]) == inf and bool(torch.isfinite(out.row_loss[1:]).all()) and bool(torch.isfinite(out.dlogits).all())
+    gm.policy_loss(x, labels, adv, out, old_logp=torch.where(old == -inf, -2.0, old), ref_logp=ref, kl_coef=0.5, mean=False)
+    q = torch.exp(lp[2] + 2.0)
+    want = -float(q * adv[2]) * (1.0 if float(q) <= 1.2 else 0.0) + 0.5
+    assert float(out.row_loss[0]) == inf and float(out.row_loss[2]) == inf
+    assert abs(float(out.dlogits[2, 9]) - want * (1 - float(torch.exp(lp[2])))) <= 1e-5 * abs(want)
+
+
 PREF = [  # V, sequence lengths, rows in front, rows behind
     (1000, [1, 1], 0, 0), (1000, [0, 5], 0, 0), (1000, [0, 0, 3, 4], 2, 3), (32000, [24, 19], 0, 2),
     (4099, [7, 130, 64, 1, 33, 65, 2, 0], 1, 0), (50, list(np.arange(66) % 9), 0, 5), (131079, [3, 2], 0, 0),
