@@ -452,6 +452,110 @@ def test_same_bits_twice_and_on_another_stream_and_in_a_graph():
         head.zero_()
 
 
+def test_two_calls_at_once_and_two_graphs_in_turn_with_buffers_of_their_own():
+    """Two streams with a LossOut each, many times over, and two captured graphs replayed on them: the bits of a call by itself."""
+    torch = gc.require_gpu()
+    V, rows = 32000, 40
+    gm = tc.head_model(V)
+    rng = np.random.default_rng(21)
+    data = [tc.make_logits(rng, rows, V, "f32") for _ in range(2)]
+    adv = torch.from_numpy(rng.standard_normal(rows).astype(np.float32)).cuda()
+    start = torch.tensor([0, 9, 20, 31, 40], dtype=torch.int32, device="cuda")
+
+    def call(i, out, kind):
+        x, labels = data[i]
+        if kind == "sar":
+            gm.sar_loss_grad(x, labels, out, mean=True)
+        elif kind == "policy":
+            gm.policy_loss(x, labels, adv, out)
+        else:
+            gm.preference_loss(x, labels, start, out)
+
+    def bits(out):
+        return [t.clone().view(torch.uint8) for t in (out.loss, out.row_logp, out.dlogits, out.n_terms)]
+
+    for kind in ("sar", "policy", "pref"):
+        want = []
+        for i in range(2):
+            out = tc.fresh_out(gm, rows, "f32", pairs=2)
+            call(i, out, kind)
+            torch.cuda.synchronize()
+            want.append(bits(out))
+        outs = [tc.fresh_out(gm, rows, "f32", pairs=2) for _ in range(2)]
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for i in range(2):
+                with torch.cuda.stream(streams[i]):
+                    call(i, outs[i], kind)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for i in range(2) for a, b in zip(want[i], bits(outs[i]))), kind
+        graphs = []
+        for i in range(2):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                call(i, outs[i], kind)
+            graphs.append(g)
+        for _ in range(3):
+            for o in outs:
+                tc.spoil(o.dlogits), tc.spoil(o.loss)
+            torch.cuda.synchronize()
+            for _ in range(5):
+                for i in range(2):
+                    with torch.cuda.stream(streams[i]):
+                        graphs[i].replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for i in range(2) for a, b in zip(want[i], bits(outs[i]))), kind
+
+
+def test_one_set_of_buffers_for_calls_of_every_kind():
+    """A LossOut that goes from call to call, loss to loss and back, with and without the mean: what a fresh one gives, bit for bit."""
+    torch = gc.require_gpu()
+    V = 1000
+    gm = tc.head_model(V)
+    rng = np.random.default_rng(5)
+    for rows in (30, 400):  # added up by the rows themselves, and by a launch behind them
+        x, labels = tc.make_logits(rng, rows, V, "bf16")
+        adv = torch.from_numpy(rng.standard_normal(rows).astype(np.float32)).cuda()
+        start = torch.tensor([0, rows // 3, rows], dtype=torch.int32, device="cuda")
+        calls = [lambda o: gm.sar_loss_grad(x, labels, o, mean=True), lambda o: gm.preference_loss(x, labels, start, o),
+                 lambda o: gm.policy_loss(x, labels, adv, o, mean=False), lambda o: gm.sar_loss_grad(x, labels, o), lambda o: gm.policy_loss(x, labels, adv, o)]
+        one = tc.fresh_out(gm, rows, "bf16", pairs=1)
+        for i in (0, 1, 2, 3, 4, 1, 0, 4, 4):
+            new = tc.fresh_out(gm, rows, "bf16", pairs=1)
+            calls[i](one), calls[i](new)
+            torch.cuda.synchronize()
+            assert all(torch.equal(getattr(one, n), getattr(new, n)) for n in ("loss", "n_terms", "row_logp", "dlogits")), (rows, i)
+            assert bool((one.work[:4] == 0).all()), "the arrival count"
+
+
+def test_rows_and_gradients_beyond_32_bit_offsets():
+    torch = gc.require_gpu()
+    from paper_2402_11809_amd import binding
+    V, rows, stride = 1001, 70, (1 << 26) + 3  # 4.7 G elements from the first row to the last
+    gm = tc.head_model(V)
+    x, labels = tc.make_logits(np.random.default_rng(9), rows, V, "bf16")
+    dense = tc.fresh_out(gm, rows, "bf16", pairs=1)
+    big = torch.zeros(rows * stride, dtype=torch.bfloat16, device="cuda")
+    far = big.view(rows, stride)[:, 17:17 + V]
+    start = torch.tensor([0, 30, 70], dtype=torch.int32, device="cuda")
+    out = tc.fresh_out(gm, rows, dlogits=far, pairs=1)
+    for call in (lambda a, o: gm.sar_loss_grad(a, labels, o), lambda a, o: gm.preference_loss(a, labels, start, o)):
+        far.copy_(x)
+        call(x, dense)
+        call(far, out)  # in place
+        torch.cuda.synchronize()
+        assert torch.equal(far, dense.dlogits) and torch.equal(out.loss, dense.loss)
+    del out, far, big
+    g = torch.ones((1 << 32) + 7, dtype=torch.bfloat16, device="cuda")
+    gs = binding.GradSet(gm, [g])
+    want = float((1 << 32) + 7) ** 0.5
+    assert abs(float(gm.grad_norm(gs)) - want) <= want * U * 1.001
+    gm.grad_clip(gs, 1.0, norm=torch.tensor([4.0], device="cuda"))
+    for part in g.split(1 << 30):
+        assert bool((part == 0.25).all())
+
+
 # ------------------------------------------------------------------------------- norm and clipping
 
 def _norm64(grads):
