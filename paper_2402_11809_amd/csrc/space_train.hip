@@ -715,10 +715,14 @@ hipError_t launch_rows(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) 
 }
 
 // Whether the rows' workgroups count and add up themselves.  That saves two launches (one where nothing has to be counted first), 3 -
-// 4 us, but every workgroup reads all labels and adds to one count, which takes 13 ns each: no matter where a row takes longer
-// (4000 rows of 32000 in fp32 167 -> 163 us, 500 in bf16 17 -> 15; 8000 in bf16 level), and less than the launches up to about 200
-// short rows (200 rows of 1000 in fp32 9.0 -> 8.2 us, 500 of them 9.3 -> 11.0, 2000 11.8 -> 30).
-bool small_call(const LossLaunch& l) { return l.rows <= 192 || (l.rows <= 4096 && (int64_t)l.vocab * (l.dtype ? 2 : 4) >= 48 * 1024); }
+// 4 us, but every workgroup reads all labels, and adds to one count, 13 ns each: the longer a row takes the less of either shows, so
+// the rows may be as many as the square of their bytes allows.  In one launch / apart, mean, all rows counting: 32000 in fp32
+// 1000 rows 47.0 / 49.9 us, 2900 134 / 138, 4000 181 / 186 (policy 189 / 185); in bf16 1000 rows 31.3 / 32.1, 2000 58.8 / 55.8,
+// 4000 114 / 100; short rows win up to about 200 (of 1000 in fp32: 200 8.2 / 9.0, 500 11.0 / 9.3, 2000 30 / 12).
+bool small_call(const LossLaunch& l) {
+    const int64_t bytes = min((int64_t)l.vocab * (l.dtype ? 2 : 4), (int64_t)1 << 20);
+    return l.rows <= 192 || (l.rows <= 4096 && ((int64_t)l.rows << 22) <= bytes * bytes);
+}
 
 template <int KIND>
 hipError_t launch_loss(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) {
