@@ -664,6 +664,8 @@ __global__ __launch_bounds__(1024) void pref_small_kernel(LossLaunch l, PrefArgs
     }
     pref_row<T, 1024>(l, row, label, slope);
 }
+// (threads: 8000 rows of 2000 in bf16 32 us with 64, 44 with 1024, statistics included; 8000 of 4000 in fp32 73 with 256, 75 with 128; 4000 of
+// 12000 in bf16 57.7 with 1024, 60.6 with 256)
 template <typename T>
 hipError_t launch_pref_gradient(const LossLaunch& l, hipStream_t s) {
     const dim3 grid(l.rows);
@@ -673,6 +675,11 @@ hipError_t launch_pref_gradient(const LossLaunch& l, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Threads and elements a thread by the row's length, so that few registers stay empty and two rows or more fit a CU (us, this / next best):
+// 6001 rows of 2000 in fp32 64 x 32 17.0, 128 x 16 20.1; of 4000 128 x 32 36.7, 64 x 64 38.9 (bf16 21.0, 20.3); 2000 rows of 5003 128 x 64
+// 15.6, 256 x 32 16.5; of 12000 256 x 64 34.8, 512 x 32 36.7 (4000 in bf16 36.6, 42.8); 4096 of 32000 512 x 64 182, 1024 x 32 209; 2000
+// of 64000 in fp32 1024 x 64 189, 512 x 128 200, in bf16 packed 512 x 128 98, unpacked 1024 x 64 107; 1000 of 128256 in bf16 packed 1024 x
+// 128 115, read twice 139, without gradient 76 and 68: statistics alone are read in pieces from there on.
 template <typename T, int KIND, bool SMALL>
 hipError_t launch_rows_of(const LossLaunch& l, const PolicyArgs& p, hipStream_t s) {
     constexpr int E = Vec<T>::N;
@@ -699,9 +706,12 @@ hipError_t launch_rows_of(const LossLaunch& l, const PolicyArgs& p, hipStream_t 
             if (l.vocab <= 512 * 128) {
                 SPACE_ROWS(512, 128, false);
                 return hipGetLastError();
-            } else if (KIND != LOSS_PREF && l.vocab <= 1024 * 128) {
-                SPACE_ROWS(1024, 128, false);
-                return hipGetLastError();
+            }
+            if constexpr (KIND != LOSS_PREF) {
+                if (l.vocab <= 1024 * 128) {
+                    SPACE_ROWS(1024, 128, false);
+                    return hipGetLastError();
+                }
             }
         }
         hipLaunchKernelGGL((loss_long_rows_kernel<T, KIND, SMALL>), grid, dim3(kLongThreads), 0, s, l, p);
@@ -950,8 +960,10 @@ hipError_t each_grad_list(const GradTensor* t, int n, F launch) {
 
 int grad_workgroups(int64_t chunks) { return (int)(chunks < kGradParts ? chunks : kGradParts); }
 
-// Workgroups up to which the last one takes the root itself: one launch less, about 3 us, against additions to one count.
-constexpr int kGradSmall = 512;
+// Workgroups up to which the last one takes the root itself: one launch less, but each adds to one count, 14 ns.  On the GPU alone that is
+// level at 128 (16 workgroups 5.8 us in one launch, 6.6 apart; 128 6.5 and 6.6, 256 8.0 and 6.6, 384 9.8 and 6.7), but a call of
+// this size waits for the host, which makes the launches: norm and clipping of 265 chunks 13.3 us in one, 14.4 apart.
+constexpr int kGradSmall = 288;
 
 hipError_t launch_grad_norm(const GradTensor* t, int n, float* norm, double* work, hipStream_t s) {
     uint32_t* arrived = (uint32_t*)work;
