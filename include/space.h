@@ -403,8 +403,8 @@ int space_policy_loss(space_ctx *ctx, const space_loss_io *io, const space_polic
  * of s that count (average: their mean; 0 for a sequence without any).
  *   z = beta * ((S_2p - ref_2p) - (S_2p+1 - ref_2p+1)) - margin
  *   term_p = (1 - smoothing) * softplus(-z) + smoothing * softplus(z)
- * Rows in front of the first and behind the last sequence do not count.  Offsets outside 0 .. rows or in falling order are
- * clamped and counted by space_device_faults(). */
+ * Rows in front of the first and behind the last sequence do not count (their row_logp is written all the same).  Offsets outside
+ * 0 .. rows or in falling order are clamped and counted by space_device_faults(); which rows a sequence then has is unspecified. */
 typedef struct space_preference_params {
     const int32_t *seq_start; /* [2 * pairs + 1] */
     const float *ref_logp;    /* [2 * pairs] S under the reference model (a mean where average is set); NULL: 0 */

@@ -395,17 +395,17 @@ def test_gradient_against_differences(kind):
         assert abs(num - want) <= 12 * 300 * U / h + 40 * h * h, (i, num, want)
 
 
-def test_same_bits_twice_and_on_another_stream_and_in_a_graph():
+@pytest.mark.parametrize("V,rows", [(32000, 40), (1000, 700), (131079, 3)])
+def test_same_bits_twice_and_on_another_stream_and_in_a_graph(V, rows):
     """Each loss and the clipping: eager twice, on a side stream, and captured and replayed with inputs that change between the replays."""
     torch = gc.require_gpu()
     from paper_2402_11809_amd import binding
-    V, rows = 32000, 40
     rng = np.random.default_rng(8)
     gm = tc.head_model(V)
     data = [tc.make_logits(rng, rows, V, "bf16") for _ in range(3)]
     x, labels = data[0][0].clone(), data[0][1].clone()
     adv = torch.from_numpy(rng.standard_normal(rows).astype(np.float32)).cuda()
-    start = torch.tensor([0, 11, 20, 33, 40], dtype=torch.int32, device="cuda")
+    start = torch.tensor([0, rows // 4, rows // 2, rows - 1, rows], dtype=torch.int32, device="cuda")
     head = torch.zeros(V, 3, device="cuda")
 
     def calls(outs, gset):
@@ -527,6 +527,40 @@ def test_one_set_of_buffers_for_calls_of_every_kind():
             torch.cuda.synchronize()
             assert all(torch.equal(getattr(one, n), getattr(new, n)) for n in ("loss", "n_terms", "row_logp", "dlogits")), (rows, i)
             assert bool((one.work[:4] == 0).all()), "the arrival count"
+
+
+@pytest.mark.parametrize("V,rows", [(1000, 1), (1000, 30), (1000, 900), (32000, 200), (131079, 3)])
+def test_loss_without_gradient_and_without_what_may_be_left_out(V, rows):
+    """dlogits NULL: the loss, terms and counts of the call with a gradient, bit for bit.  row_kl, n_clipped and seq_logp NULL: the rest as it was."""
+    torch = gc.require_gpu()
+    from paper_2402_11809_amd import binding
+    gm = tc.head_model(V)
+    rng = np.random.default_rng(rows)
+    x, labels = tc.make_logits(rng, rows, V, "f32")
+    adv = torch.from_numpy(rng.standard_normal(rows).astype(np.float32)).cuda()
+    start = torch.tensor([0, rows // 3, rows], dtype=torch.int32, device="cuda")
+    full, bare = tc.fresh_out(gm, rows, "f32", pairs=1), tc.fresh_out(gm, rows, pairs=1)
+    for mean in (False, True):
+        for call, names in ((lambda o: gm.sar_loss_grad(x, labels, o, mean=mean), ("loss", "n_terms", "row_loss", "row_logp")),
+                            (lambda o: gm.policy_loss(x, labels, adv, o, old_logp=adv - 7, ref_logp=adv - 8, kl_coef=0.1, mean=mean),
+                             ("loss", "n_terms", "row_loss", "row_logp", "row_kl", "n_clipped")),
+                            (lambda o: gm.preference_loss(x, labels, start, o, mean=mean), ("loss", "n_terms", "row_logp", "pair_loss", "seq_logp"))):
+            call(full), call(bare)
+            torch.cuda.synchronize()
+            for n in names:
+                assert torch.equal(getattr(full, n), getattr(bare, n)), n
+    grad = full.dlogits.clone()
+    tc.spoil(full.dlogits)
+    io = gm._loss_io(x, labels, full, None, True)
+    p = binding.SpacePreferenceParams(start.data_ptr(), None, full.pair_loss.data_ptr(), None, 1, 0, 0.1, 0.0, 0.0)
+    assert gm.lib.space_preference_loss(gm.ctx, C.byref(io), C.byref(p), binding._stream()) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(full.dlogits, grad) and torch.equal(full.loss, bare.loss)
+    gm.policy_loss(x, labels, adv, bare)
+    p = binding.SpacePolicyParams(adv.data_ptr(), None, None, None, None, None, 0.2, 0.2, 0.0)
+    assert gm.lib.space_policy_loss(gm.ctx, C.byref(io), C.byref(p), binding._stream()) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(full.loss, bare.loss) and torch.equal(full.row_loss, bare.row_loss)
 
 
 def test_rows_and_gradients_beyond_32_bit_offsets():
