@@ -616,7 +616,7 @@ int grad_list(space_ctx* ctx, const char* who, const space_grad_tensor* t, int32
     for (int32_t i = 0; i < n; ++i) {
         const size_t gb = dtype_bytes(t[i].dtype), ob = dtype_bytes(t[i].out_dtype);
         if (!gb || (writes && !ob)) return fail(ctx, SPACE_EINVAL, "%s: tensor %d: unknown dtype", who, i);
-        if (t[i].n < 0 || t[i].n > INT64_MAX / 8) return fail(ctx, SPACE_EINVAL, "%s: tensor %d: length %lld", who, i, (long long)t[i].n);
+        if (t[i].n < 0 || t[i].n > (int64_t)1 << 42) return fail(ctx, SPACE_EINVAL, "%s: tensor %d: length %lld", who, i, (long long)t[i].n);
         (*list)[i] = GradTensor{t[i].grad, writes ? t[i].out : nullptr, t[i].n, t[i].dtype, writes ? t[i].out_dtype : t[i].dtype};
         if (t[i].n == 0) continue;
         const uintptr_t g = (uintptr_t)t[i].grad, o = (uintptr_t)t[i].out;

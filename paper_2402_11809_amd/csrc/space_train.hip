@@ -771,20 +771,19 @@ hipError_t launch_preference(const LossLaunch& l, const PrefArgs& p, hipStream_t
 // ------------------------------------------------------------------------------------------
 // gradient norm and clipping
 // ------------------------------------------------------------------------------------------
-// A launch takes up to kGradList tensors by value (arguments of a kernel: 4 KB at most), so nothing has to be kept on the device; their elements are cut into
-// chunks that are dealt out to the workgroups in turn.
-constexpr int kGradList = 112, kGradThreads = 256, kGradChunk = kGradThreads * 32;
+// A launch takes up to kGradList tensors by value (arguments of a kernel: 4 KB at most), so nothing has to be kept on the device; their
+// elements are cut into chunks that are dealt out to the workgroups in turn.
+constexpr int kGradList = 152, kGradThreads = 256, kGradChunk = kGradThreads * 32, kGradChunks = 1 << 30;
 struct GradList {
     const void* grad[kGradList];
     void* out[kGradList];
-    int64_t n[kGradList];
-    int64_t first[kGradList + 1];  // chunks in front of a tensor
-    uint8_t type[kGradList];       // bit 0: bf16 gradient, bit 1: bf16 output
+    int32_t first[kGradList + 1];  // chunks in front of a tensor, up to kGradChunks
+    int32_t last[kGradList];       // elements of its last chunk; bit 14: bf16 gradient, bit 15: bf16 output (16 bits would take a vector load)
     int count;
 };
-static_assert(sizeof(GradList) < 3900, "arguments of a kernel");
+static_assert(sizeof(GradList) <= 3700 && kGradChunk < 1 << 14, "arguments of a kernel, elements of a chunk");
 
-__device__ __forceinline__ int grad_tensor_of(const GradList& g, int64_t chunk) {
+__device__ __forceinline__ int grad_tensor_of(const GradList& g, int chunk) {
     int lo = 0, hi = g.count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -792,6 +791,7 @@ __device__ __forceinline__ int grad_tensor_of(const GradList& g, int64_t chunk) 
     }
     return lo;
 }
+__device__ __forceinline__ int chunk_elements(const GradList& g, int t, int chunk) { return chunk + 1 < g.first[t + 1] ? kGradChunk : g.last[t] & 0x3fff; }
 
 // What both passes over the gradients read twice comes from the memory-side cache the second time, if it is small enough: the
 // last kGradKept bytes are read in the ordinary way by the norm, and first by the clipping; everything in front of them, which the
@@ -827,13 +827,12 @@ __device__ __forceinline__ double chunk_squares(const T* __restrict__ x, int n) 
 
 // One chunk after another, dealt out to the workgroups; those from kept_from on stay in the cache.
 template <bool KEPT>
-__device__ __forceinline__ double list_squares(const GradList& g, int64_t c, int64_t end) {
+__device__ __forceinline__ double list_squares(const GradList& g, int c, int end) {
     double sum = 0.0;
     for (; c < end; c += gridDim.x) {
-        const int t = grad_tensor_of(g, c);
-        const int64_t from = (c - g.first[t]) * kGradChunk;
-        const int n = (int)min((int64_t)kGradChunk, g.n[t] - from);
-        if (g.type[t] & 1) sum += chunk_squares<uint16_t, KEPT>((const uint16_t*)g.grad[t] + from, n);
+        const int t = grad_tensor_of(g, c), n = chunk_elements(g, t, c);
+        const int64_t from = (int64_t)(c - g.first[t]) * kGradChunk;
+        if (g.last[t] & 0x4000) sum += chunk_squares<uint16_t, KEPT>((const uint16_t*)g.grad[t] + from, n);
         else sum += chunk_squares<float, KEPT>((const float*)g.grad[t] + from, n);
     }
     return sum;
@@ -846,13 +845,14 @@ __device__ __forceinline__ void sum_squares(const double* work, int parts, float
     if (threadIdx.x == 0) *norm = (float)sqrt(sum);
 }
 // arrived: a lone launch of few workgroups, the last of which takes the root; else a launch behind them does
-__global__ __launch_bounds__(kGradThreads) void grad_square_kernel(GradList g, int64_t kept_from, double* work, int first_launch, uint32_t* arrived,
+__global__ __launch_bounds__(kGradThreads) void grad_square_kernel(GradList g, int kept_from, double* work, int first_launch, uint32_t* arrived,
                                                                    float* norm) {
     __shared__ double s[kGradThreads / 64];
     __shared__ int s_last;
-    double sum = list_squares<false>(g, blockIdx.x, kept_from);
-    const int64_t turn = (kept_from + gridDim.x - 1 - blockIdx.x) / gridDim.x;  // how many of those this workgroup had
-    sum += list_squares<true>(g, blockIdx.x + turn * gridDim.x, g.first[g.count]);
+    const int mine = blockIdx.x, step = gridDim.x;
+    double sum = list_squares<false>(g, mine, kept_from);
+    const int turns = max(kept_from - mine + step - 1, 0) / step;  // how many of those this workgroup had
+    sum += list_squares<true>(g, mine + turns * step, g.first[g.count]);
     sum = block_sum<kGradThreads / 64>(sum, s);
     if (threadIdx.x == 0) __hip_atomic_store(work + blockIdx.x, first_launch ? sum : work[blockIdx.x] + sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (arrived && arrive(arrived, &s_last)) sum_squares<kGradThreads, true>(work, gridDim.x, norm, s);
@@ -862,15 +862,11 @@ __global__ __launch_bounds__(1024) void grad_norm_kernel(const double* work, int
     sum_squares<1024, false>(work, parts, norm, s);
 }
 
-// N elements as a thread reads or writes them: 16 bytes, or 8 where bf16 goes with fp32, so that neighbouring lanes' stores meet
-template <typename T, int N> struct Some {
-    template <bool KEPT> static __device__ __forceinline__ void load(const T* p, float* v) { Vec<T>::get(read_vec<KEPT, Vec<T>>(p), v); }
-    static __device__ __forceinline__ void store(T* p, const float* v) { __builtin_nontemporal_store(Vec<T>::put(v), (typename Vec<T>::raw*)p); }
-};
-template <> struct Some<uint16_t, 4> {
+// Four bf16 numbers, which go with four in fp32: neighbouring lanes' stores meet
+struct Vec4Bf16 {
+    static constexpr int N = 4;
     typedef uint32_t raw __attribute__((ext_vector_type(2), aligned(2)));
-    template <bool KEPT> static __device__ __forceinline__ void load(const uint16_t* p, float* v) {
-        const raw q = read_vec<KEPT, Some>(p);
+    static __device__ __forceinline__ void get(raw q, float* v) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const uint32_t w = q[e];
@@ -878,44 +874,57 @@ template <> struct Some<uint16_t, 4> {
             v[2 * e + 1] = __uint_as_float(w & 0xffff0000u);
         }
     }
-    static __device__ __forceinline__ void store(uint16_t* p, const float* v) {
+    static __device__ __forceinline__ raw put(const float* v) {
         raw q;
 #pragma unroll
         for (int e = 0; e < 2; ++e) q[e] = (uint32_t)f2bf(v[2 * e]) | (uint32_t)f2bf(v[2 * e + 1]) << 16;
-        __builtin_nontemporal_store(q, (raw*)p);
+        return q;
     }
 };
-// n elements of a chunk, scaled
+template <typename T, typename Other> struct VecBeside { typedef Vec<T> type; };
+template <> struct VecBeside<uint16_t, float> { typedef Vec4Bf16 type; };
+
+// n elements of a chunk, scaled.  (All loads, then all arithmetic, then all stores: what stands in one condition with a load or a store
+// waits for it, one vector after the other: 667 M bf16 gradients into fp32 932 -> 905 us.)
 template <bool KEPT, typename T, typename O>
 __device__ __forceinline__ void chunk_scale(const T* x, O* y, int n, float scale) {
-    constexpr int E = sizeof(T) == 2 && sizeof(O) == 2 ? 8 : 4, NV = kGradChunk / kGradThreads / E;
+    typedef typename VecBeside<T, O>::type In;
+    typedef typename VecBeside<O, T>::type Out;
+    constexpr int E = In::N, NV = kGradChunk / kGradThreads / E;
+    static_assert(In::N == Out::N, "as many elements in as out");
     const int tid = threadIdx.x, whole = n / E, odd = whole * E + tid;
-    float v[NV][E];
+    typename In::raw q[NV];
+    typename Out::raw r[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-        if (tid + j * kGradThreads < whole) Some<T, E>::template load<KEPT>(x + (tid + j * kGradThreads) * E, v[j]);
+    for (int j = 0; j < NV; ++j) {
+        q[j] = typename In::raw{};
+        if (tid + j * kGradThreads < whole) q[j] = read_vec<KEPT, In>(x + (tid + j * kGradThreads) * E);
+    }
     if (odd < n) store_f32(y + odd, load_f32(x + odd) * scale);
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-        if (tid + j * kGradThreads < whole) {
+    for (int j = 0; j < NV; ++j) {
+        float v[E];
+        In::get(q[j], v);
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[j][e] *= scale;
-            Some<O, E>::store(y + (tid + j * kGradThreads) * E, v[j]);
-        }
+        for (int e = 0; e < E; ++e) v[e] *= scale;
+        r[j] = Out::put(v);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (tid + j * kGradThreads < whole) __builtin_nontemporal_store(r[j], (typename Out::raw*)(y + (tid + j * kGradThreads) * E));
 }
 
 template <bool KEPT>
-__global__ __launch_bounds__(kGradThreads) void grad_clip_kernel(GradList g, int64_t begin, int64_t end, const float* norm, float max_norm) {
-    const float n = *norm;
-    const float scale = n > max_norm && n < INFINITY ? max_norm / n : 1.f;
-    for (int64_t c = begin + blockIdx.x; c < end; c += gridDim.x) {
-        const int t = grad_tensor_of(g, c);
+__global__ __launch_bounds__(kGradThreads) void grad_clip_kernel(GradList g, int begin, int end, const float* norm, float max_norm) {
+    const float size = *norm;
+    const float scale = size > max_norm && size < INFINITY ? max_norm / size : 1.f;
+    for (int c = begin + blockIdx.x; c < end; c += gridDim.x) {
+        const int t = grad_tensor_of(g, c), n = chunk_elements(g, t, c);
         if (scale == 1.f && g.out[t] == g.grad[t]) continue;
-        const int64_t from = (c - g.first[t]) * kGradChunk;
-        const int n = (int)min((int64_t)kGradChunk, g.n[t] - from);
+        const int64_t from = (int64_t)(c - g.first[t]) * kGradChunk;
         const void* x = g.grad[t];
         void* y = g.out[t];
-        switch (g.type[t]) {
+        switch (g.last[t] >> 14) {
             case 0: chunk_scale<KEPT>((const float*)x + from, (float*)y + from, n, scale); break;
             case 1: chunk_scale<KEPT>((const uint16_t*)x + from, (float*)y + from, n, scale); break;
             case 2: chunk_scale<KEPT>((const float*)x + from, (uint16_t*)y + from, n, scale); break;
@@ -926,7 +935,7 @@ __global__ __launch_bounds__(kGradThreads) void grad_clip_kernel(GradList g, int
 
 int64_t grad_bytes(const GradTensor& t) { return t.n * (t.dtype ? 2 : 4); }
 
-// Calls launch(list, first chunk that is kept) for every kGradList tensors that are not empty.
+// Calls launch(list, first chunk that is kept) for every kGradList tensors that are not empty (fewer where they have too many chunks).
 template <typename F>
 hipError_t each_grad_list(const GradTensor* t, int n, F launch) {
     int64_t left = -kGradKept;  // bytes still in front of those that are kept
@@ -935,19 +944,19 @@ hipError_t each_grad_list(const GradTensor* t, int n, F launch) {
     for (int i = 0; i < n;) {
         g.count = 0;
         g.first[0] = 0;
-        int64_t kept_from = 0;
+        int kept_from = 0;
         for (; i < n && g.count < kGradList; ++i) {
             if (t[i].n == 0) continue;
+            const int64_t chunks = (t[i].n + kGradChunk - 1) / kGradChunk;
+            if (g.first[g.count] + chunks > kGradChunks) break;  // (a lone tensor has fewer: grad_list)
             const int c = g.count++;
             g.grad[c] = t[i].grad;
             g.out[c] = t[i].out;
-            g.n[c] = t[i].n;
-            g.type[c] = (uint8_t)(t[i].dtype | t[i].out_dtype << 1);
-            const int64_t chunks = (t[i].n + kGradChunk - 1) / kGradChunk;
-            g.first[c + 1] = g.first[c] + chunks;
+            g.last[c] = (int)(t[i].n - (chunks - 1) * kGradChunk) | t[i].dtype << 14 | t[i].out_dtype << 15;
+            g.first[c + 1] = g.first[c] + (int)chunks;
             if (left > 0) {
-                const int64_t past = (left + kGradChunk * (t[i].dtype ? 2 : 4) - 1) / (kGradChunk * (t[i].dtype ? 2 : 4));
-                kept_from = g.first[c] + (past < chunks ? past : chunks);
+                const int64_t bytes = kGradChunk * (t[i].dtype ? 2 : 4), past = (left + bytes - 1) / bytes;
+                kept_from = g.first[c] + (int)(past < chunks ? past : chunks);
             }
             left -= grad_bytes(t[i]);
         }
@@ -958,7 +967,7 @@ hipError_t each_grad_list(const GradTensor* t, int n, F launch) {
     return hipSuccess;
 }
 
-int grad_workgroups(int64_t chunks) { return (int)(chunks < kGradParts ? chunks : kGradParts); }
+int grad_workgroups(int chunks) { return chunks < kGradParts ? chunks : kGradParts; }
 
 // Workgroups up to which the last one takes the root itself: one launch less, but each adds to one count, 14 ns.  On the GPU alone that is
 // level at 128 (16 workgroups 5.8 us in one launch, 6.6 apart; 128 6.5 and 6.6, 256 8.0 and 6.6, 384 9.8 and 6.7), but a call of
@@ -970,13 +979,13 @@ hipError_t launch_grad_norm(const GradTensor* t, int n, float* norm, double* wor
     work += 2;
     // a later launch adds to the partial sums of an earlier one, so all of them have as many workgroups
     int parts = 0, lists = 0, first = 1;
-    hipError_t e = each_grad_list(t, n, [&](const GradList& g, int64_t) {
+    hipError_t e = each_grad_list(t, n, [&](const GradList& g, int) {
         parts = max(parts, grad_workgroups(g.first[g.count]));
         ++lists;
     });
     if (e != hipSuccess) return e;
     const bool small = lists == 1 && parts <= kGradSmall;
-    e = each_grad_list(t, n, [&](const GradList& g, int64_t kept_from) {
+    e = each_grad_list(t, n, [&](const GradList& g, int kept_from) {
         hipLaunchKernelGGL(grad_square_kernel, dim3(parts), dim3(kGradThreads), 0, s, g, kept_from, work, first, small ? arrived : nullptr, norm);
         first = 0;
     });
@@ -986,13 +995,13 @@ hipError_t launch_grad_norm(const GradTensor* t, int n, float* norm, double* wor
 }
 
 hipError_t launch_grad_clip(const GradTensor* t, int n, const float* norm, float max_norm, hipStream_t s) {
-    const hipError_t e = each_grad_list(t, n, [&](const GradList& g, int64_t kept_from) {
-        const int64_t end = g.first[g.count];
+    const hipError_t e = each_grad_list(t, n, [&](const GradList& g, int kept_from) {
+        const int end = g.first[g.count];
         if (kept_from < end) hipLaunchKernelGGL(grad_clip_kernel<true>, dim3(grad_workgroups(end - kept_from)), dim3(kGradThreads), 0, s, g, kept_from, end, norm, max_norm);
     });
     if (e != hipSuccess) return e;
-    return each_grad_list(t, n, [&](const GradList& g, int64_t kept_from) {
-        if (kept_from > 0) hipLaunchKernelGGL(grad_clip_kernel<false>, dim3(grad_workgroups(kept_from)), dim3(kGradThreads), 0, s, g, (int64_t)0, kept_from, norm, max_norm);
+    return each_grad_list(t, n, [&](const GradList& g, int kept_from) {
+        if (kept_from > 0) hipLaunchKernelGGL(grad_clip_kernel<false>, dim3(grad_workgroups(kept_from)), dim3(kGradThreads), 0, s, g, 0, kept_from, norm, max_norm);
     });
 }
 

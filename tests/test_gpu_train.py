@@ -636,7 +636,7 @@ def test_more_gradients_than_the_cache_holds_over_several_launches():
     torch = gc.require_gpu()
     from paper_2402_11809_amd import binding
     gm = tc.head_model(40)
-    sizes = [(1 << 20) + 3 * i for i in range(118)]
+    sizes = [(5 << 17) + 3 * i for i in range(190)]
     for types, value in ((["f32"], 0.5), (["f32", "bf16"], 1.0), (["bf16"], 0.25)):
         grads = [torch.full((n,), value, dtype=tc.torch_type(types[i % len(types)]), device="cuda") for i, n in enumerate(sizes)]
         want = value * sum(sizes) ** 0.5
