@@ -363,9 +363,9 @@ __device__ __forceinline__ double slope_factor(const LossLaunch& l, int n) {
 }
 // The slope with everything in it, for all threads; the policy loss has it from thread 0.
 template <int KIND>
-__device__ __forceinline__ float row_coefficient(const LossLaunch& l, const PolicyArgs& p, int row, const RowFacts& f, float x_label, int n, float* s_slope) {
-    if (KIND == LOSS_SAR) return (float)-slope_factor(l, n);
-    if (threadIdx.x == 0) *s_slope = (float)(row_outputs<KIND>(l, p, row, f, x_label) * slope_factor(l, n));
+__device__ __forceinline__ double row_coefficient(const LossLaunch& l, const PolicyArgs& p, int row, const RowFacts& f, float x_label, int n, double* s_slope) {
+    if (KIND == LOSS_SAR) return -slope_factor(l, n);
+    if (threadIdx.x == 0) *s_slope = row_outputs<KIND>(l, p, row, f, x_label) * slope_factor(l, n);
     __syncthreads();
     return *s_slope;
 }
@@ -388,8 +388,8 @@ template <typename T, int KIND, int THREADS, int NV, bool KEEP, bool SMALL>
 __device__ __forceinline__ void row_of_loss(const LossLaunch& l, const PolicyArgs& p) {
     typedef Vec<T> V;
     constexpr int W = THREADS / 64, E = V::N;
-    __shared__ float s_max[W], s_slope;
-    __shared__ double s_sum[W];
+    __shared__ float s_max[W];
+    __shared__ double s_sum[W], s_slope;
     __shared__ int s_n[W];
     const int row = blockIdx.x, tid = threadIdx.x, label = l.labels[row], vocab = l.vocab;
     const T* x = (const T*)l.logits + (size_t)row * l.logits_stride;
@@ -459,8 +459,9 @@ __device__ __forceinline__ void row_of_loss(const LossLaunch& l, const PolicyArg
         return;
     }
     const int n = !l.mean ? 1 : SMALL ? sum_of<W>(s_n) : *l.n_terms;
-    const float c = row_coefficient<KIND>(l, p, row, f, x_label, n, &s_slope);
-    const float inv = 1.f / (float)f.total, per_e = -c * inv * factor, at_label = c * ((float)f.others / (float)f.total);
+    // (what a row's elements are multiplied with is rounded once)
+    const double c = row_coefficient<KIND>(l, p, row, f, x_label, n, &s_slope) / f.total;
+    const float per_e = (float)(-c * factor), at_label = (float)(c * f.others);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
         if (tid + j * THREADS < whole) {
@@ -525,8 +526,8 @@ template <typename T, int KIND, bool SMALL>
 __device__ __forceinline__ void long_row_of_loss(const LossLaunch& l, const PolicyArgs& p) {
     typedef Vec<T> V;
     constexpr int W = kLongThreads / 64, E = V::N;
-    __shared__ float s_max[W], s_slope;
-    __shared__ double s_sum[W];
+    __shared__ float s_max[W];
+    __shared__ double s_sum[W], s_slope;
     __shared__ int s_n[W];
     const int row = blockIdx.x, tid = threadIdx.x, label = l.labels[row], vocab = l.vocab;
     const T* x = (const T*)l.logits + (size_t)row * l.logits_stride;
@@ -585,9 +586,8 @@ __device__ __forceinline__ void long_row_of_loss(const LossLaunch& l, const Poli
         return;
     }
     const int n = !l.mean ? 1 : SMALL ? sum_of<W>(s_n) : *l.n_terms;
-    const float c = row_coefficient<KIND>(l, p, row, f, x_label, n, &s_slope);
-    const float inv = 1.f / (float)f.total;
-    long_gradient<T, kLongThreads>(x, d, vocab, label, f.top, -c * inv, c * ((float)f.others / (float)f.total));
+    const double c = row_coefficient<KIND>(l, p, row, f, x_label, n, &s_slope) / f.total;
+    long_gradient<T, kLongThreads>(x, d, vocab, label, f.top, (float)-c, (float)(c * f.others));
     if (KIND == LOSS_SAR && tid == 0) row_outputs<KIND>(l, p, row, f, x_label);
 }
 
