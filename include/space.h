@@ -352,7 +352,9 @@ int space_sar_loss(space_ctx *ctx, const float *logits, const int32_t *labels, i
  *   - all scratch is the caller's (row_logp, row_loss, work): calls with buffers of their own may overlap in time; two calls
  *     that share `work` or an output must be ordered, or their outputs are spoiled (those of later calls are not).
  * All pointers are DEVICE.  Elements between vocab and a row's stride are neither read nor written.  dlogits may be
- * logits itself (same pointer and stride); otherwise the two must not overlap. */
+ * logits itself (same pointer and stride); otherwise the two must not overlap.  Neither may any other output or `work` overlap
+ * an input or another output: an earlier call's row_logp that is to be old_logp or ref_logp, or its seq_logp that is to be
+ * ref_logp, is copied first or comes from outputs of another call. */
 typedef enum space_dtype { SPACE_F32 = 0, SPACE_BF16 = 1 } space_dtype;
 
 typedef struct space_loss_io {
@@ -378,7 +380,8 @@ typedef struct space_loss_io {
 
 /* The loss of space_sar_loss with its gradient: term_r = -logp_r.  Asynchronous on `stream`, no allocation.
  * Errors of all three: SPACE_EINVAL (null pointer, rows < 1, stride below vocab, unknown dtype, an array that is not on its
- * element's size, dlogits overlapping logits, a parameter out of its range), SPACE_ESHAPE (rows or pairs >= 4194304). */
+ * element's size, dlogits overlapping logits, an output or `work` overlapping another array, a parameter out of its range),
+ * SPACE_ESHAPE (rows or pairs >= 4194304). */
 int space_sar_loss_grad(space_ctx *ctx, const space_loss_io *io, void *stream);
 
 /* Clipped policy loss with a KL term, for rollouts of this model (labels = the tokens that were generated):

@@ -331,7 +331,8 @@ class LossOut:
     """Device buffers for the outputs and the scratch of sar_loss_grad, policy_loss and preference_loss, allocated once and
     reused: `rows` rows of logits, `pairs` pairs (preference_loss).  grad_dtype: the logits' type, for a gradient `dlogits`
     [rows, vocab] of its own; or dlogits: a tensor of the caller's with unit column stride (the logits themselves, too);
-    neither: no gradient.  Two calls that may overlap in time need a LossOut each."""
+    neither: no gradient.  Two calls that may overlap in time need a LossOut each.  A call takes none of its own outputs as an input:
+    row_logp or seq_logp of an earlier one goes in as a clone, or from a LossOut of its own."""
 
     def __init__(self, model: "Model", rows: int, grad_dtype=None, dlogits=None, pairs: int = 0):
         import torch

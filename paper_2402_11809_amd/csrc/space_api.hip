@@ -572,8 +572,30 @@ bool words(std::initializer_list<const void*> ptrs) {  // on 4 bytes (or null)
     return true;
 }
 
-// The checks that the losses share, and their common arguments as the kernels take them.
-int loss_launch(space_ctx* ctx, const char* who, const space_loss_io* io, bool row_terms, LossLaunch* l) {
+// The arrays of a loss beside logits and gradient.  What the rows' workgroups write while others still read may not be an input of
+// the same call, and no two outputs may share a byte.
+struct LossArrays {
+    ByteRange r[20];
+    size_t n = 0;
+    void add(const void* p, int64_t count, bool written, size_t bytes = 4) {
+        if (p) r[n++] = ByteRange{(uintptr_t)p, (uintptr_t)p + (uintptr_t)count * bytes, written};
+    }
+    void in(const void* p, int64_t count) { add(p, count, false); }
+    void out(const void* p, int64_t count) { add(p, count, true); }
+};
+int loss_arrays_apart(space_ctx* ctx, const char* who, const LossLaunch& l, LossArrays* a) {
+    const size_t b = dtype_bytes(l.dtype);
+    bool apart = written_apart(a->r, a->n);
+    for (size_t i = 0; i < a->n && apart; ++i) {
+        const ByteRange& q = a->r[i];
+        apart = !(q.written && rows_meet((uintptr_t)l.logits, l.logits_stride, l.rows, l.vocab, b, q.lo, q.hi)) &&
+                !(l.dlogits && rows_meet((uintptr_t)l.dlogits, l.dlogits_stride, l.rows, l.vocab, b, q.lo, q.hi));
+    }
+    return apart ? SPACE_OK : fail(ctx, SPACE_EINVAL, "%s: an output or the scratch overlaps another array of the call", who);
+}
+
+// The checks that the losses share, and their common arguments as the kernels take them; their arrays go to `a`.
+int loss_launch(space_ctx* ctx, const char* who, const space_loss_io* io, bool row_terms, LossLaunch* l, LossArrays* a) {
     if (!io || !io->logits || !io->labels || !io->loss || !io->n_terms || !io->row_logp || !io->work || (row_terms && !io->row_loss))
         return fail(ctx, SPACE_EINVAL, "%s: null argument", who);
     const int vocab = ctx->cfg.vocab;
@@ -601,6 +623,13 @@ int loss_launch(space_ctx* ctx, const char* who, const space_loss_io* io, bool r
     l->logits_stride = io->logits_stride; l->dlogits_stride = io->dlogits_stride;
     l->rows = io->rows; l->vocab = vocab; l->dtype = io->dtype; l->mean = io->mean != 0;
     l->faults = ctx->faults;
+    a->in(io->labels, io->rows);
+    a->in(io->grad_scale, 1);
+    a->out(io->loss, 1);
+    a->out(io->n_terms, 1);
+    a->out(io->row_logp, io->rows);
+    if (row_terms) a->out(io->row_loss, io->rows);
+    a->add(io->work, (int64_t)io->rows + 1, true, SPACE_LOSS_WORK);
     return SPACE_OK;
 }
 
@@ -1209,8 +1238,11 @@ int space_sar_transform(const int32_t* tokens, int32_t n_prompt, int32_t n_answe
 
 int space_sar_loss_grad(space_ctx* ctx, const space_loss_io* io, void* stream) {
     if (!ctx) return SPACE_EINVAL;
+    const char* who = "space_sar_loss_grad";
     LossLaunch l;
-    if (int rc = loss_launch(ctx, "space_sar_loss_grad", io, true, &l)) return rc;
+    LossArrays a;
+    if (int rc = loss_launch(ctx, who, io, true, &l, &a)) return rc;
+    if (int rc = loss_arrays_apart(ctx, who, l, &a)) return rc;
     HIP_TRY(ctx, launch_sar_grad(l, (hipStream_t)stream));
     return SPACE_OK;
 }
@@ -1219,7 +1251,8 @@ int space_policy_loss(space_ctx* ctx, const space_loss_io* io, const space_polic
     if (!ctx) return SPACE_EINVAL;
     const char* who = "space_policy_loss";
     LossLaunch l;
-    if (int rc = loss_launch(ctx, who, io, true, &l)) return rc;
+    LossArrays a;
+    if (int rc = loss_launch(ctx, who, io, true, &l, &a)) return rc;
     if (!params || !params->advantages) return fail(ctx, SPACE_EINVAL, "%s: null argument", who);
     if (!(params->clip_low >= 0.f && params->clip_low <= 1.f) || !(params->clip_high >= 0.f) || !std::isfinite(params->clip_high) ||
         !(params->kl_coef >= 0.f) || !std::isfinite(params->kl_coef))
@@ -1228,6 +1261,10 @@ int space_policy_loss(space_ctx* ctx, const space_loss_io* io, const space_polic
     if (!words({params->advantages, params->old_logp, params->ref_logp, params->row_weight, params->row_kl, params->n_clipped}))
         return fail(ctx, SPACE_EINVAL, "%s: an array not on 4 bytes", who);
     if (params->kl_coef != 0.f && !params->ref_logp) return fail(ctx, SPACE_EINVAL, "%s: kl_coef needs ref_logp", who);
+    for (const float* q : {params->advantages, params->old_logp, params->ref_logp, params->row_weight}) a.in(q, l.rows);
+    a.out(params->row_kl, l.rows);
+    a.out(params->n_clipped, 1);
+    if (int rc = loss_arrays_apart(ctx, who, l, &a)) return rc;
     PolicyArgs p{};
     p.advantages = params->advantages; p.old_logp = params->old_logp; p.ref_logp = params->ref_logp;
     p.row_weight = params->row_weight; p.row_kl = params->row_kl; p.n_clipped = params->n_clipped;
@@ -1240,7 +1277,8 @@ int space_preference_loss(space_ctx* ctx, const space_loss_io* io, const space_p
     if (!ctx) return SPACE_EINVAL;
     const char* who = "space_preference_loss";
     LossLaunch l;
-    if (int rc = loss_launch(ctx, who, io, false, &l)) return rc;
+    LossArrays a;
+    if (int rc = loss_launch(ctx, who, io, false, &l, &a)) return rc;
     if (!params || !params->seq_start || !params->pair_loss) return fail(ctx, SPACE_EINVAL, "%s: null argument", who);
     if (params->pairs < 1) return fail(ctx, SPACE_EINVAL, "%s: %d pairs", who, params->pairs);
     if (params->pairs > kLossRows) return fail(ctx, SPACE_ESHAPE, "%s: %d pairs, more than %d", who, params->pairs, kLossRows);
@@ -1249,6 +1287,12 @@ int space_preference_loss(space_ctx* ctx, const space_loss_io* io, const space_p
     if (!(params->beta > 0.f) || !std::isfinite(params->beta) || !std::isfinite(params->margin) || !(params->smoothing >= 0.f && params->smoothing <= 1.f))
         return fail(ctx, SPACE_EINVAL, "%s: beta %g not above 0, margin %g not finite or smoothing %g outside 0..1", who,
                     (double)params->beta, (double)params->margin, (double)params->smoothing);
+    const int64_t pairs = params->pairs;
+    a.in(params->seq_start, 2 * pairs + 1);
+    a.in(params->ref_logp, 2 * pairs);
+    a.out(params->pair_loss, pairs);
+    a.out(params->seq_logp, 2 * pairs);
+    if (int rc = loss_arrays_apart(ctx, who, l, &a)) return rc;
     PrefArgs p{};
     p.seq_start = params->seq_start; p.ref_logp = params->ref_logp; p.pair_loss = params->pair_loss; p.seq_logp = params->seq_logp;
     p.pairs = params->pairs; p.average = params->average != 0;

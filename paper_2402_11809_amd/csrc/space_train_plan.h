@@ -17,6 +17,13 @@ inline bool rows_apart(uintptr_t x, int64_t xs, uintptr_t d, int64_t ds, int64_t
     return xs == ds && off >= (uintptr_t)cols && (uintptr_t)xs - off >= (uintptr_t)cols;
 }
 
+// Whether rows of `cols` elements of `bytes` at x (stride xs elements) have a byte of lo .. hi - 1.
+inline bool rows_meet(uintptr_t x, int64_t xs, int64_t rows, int64_t cols, size_t bytes, uintptr_t lo, uintptr_t hi) {
+    const uintptr_t step = (uintptr_t)xs * bytes, len = (uintptr_t)cols * bytes;
+    const uintptr_t r = lo < x + len ? 0 : (lo - x - len) / step + 1;  // the first row that ends behind lo
+    return r < (uintptr_t)rows && x + r * step < hi;
+}
+
 struct ByteRange {
     uintptr_t lo, hi;
     bool written;

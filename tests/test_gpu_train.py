@@ -905,3 +905,59 @@ def test_lowest_value_as_a_mask_in_the_loss_without_gradient():
         gm.sar_loss(x.masked_fill(mask, value), labels, t)
     torch.cuda.synchronize()
     assert bool(torch.isfinite(got[0]).all()) and torch.equal(*got)
+
+
+# ------------------------------------------------------------------------------- what may not overlap
+
+def test_outputs_of_a_loss_on_its_inputs_or_on_each_other_are_refused():
+    """Values of an earlier call go in as a copy: a call that gets its own outputs as inputs (whose values it would have spoiled) is refused,
+    and so are two outputs, or the scratch, on the same bytes."""
+    torch = gc.require_gpu()
+    from paper_2402_11809_amd import binding
+    V, rows = 100, 4
+    gm = tc.head_model(V)
+    x, labels = tc.make_logits(np.random.default_rng(6), rows, V, "f32")
+    labels.fill_(3)
+    adv = torch.tensor([1.0, -1.0, 0.5, -0.5], device="cuda")
+    start = torch.tensor([0, 1, 2, 3, 4], dtype=torch.int32, device="cuda")
+    out = tc.fresh_out(gm, rows, "f32", pairs=2)
+    refused = lambda call: pytest.raises(binding.SpaceError, call)
+
+    gm.policy_loss(x, labels, adv, out)
+    old, ref = out.row_logp.clone(), out.row_logp - 0.5
+    for kw in (dict(old_logp=out.row_logp), dict(ref_logp=out.row_logp, kl_coef=0.1), dict(old_logp=out.row_loss), dict(row_weight=out.row_kl),
+               dict(old_logp=out.work[4:8]), dict(grad_scale=out.loss), dict(ref_logp=out.dlogits[1, :4])):
+        refused(lambda: gm.policy_loss(x, labels, adv, out, **kw))
+    refused(lambda: gm.policy_loss(x, labels, out.row_logp, out))
+    refused(lambda: gm.sar_loss_grad(x, out.row_logp.view(torch.int32), out))
+    refused(lambda: gm.sar_loss_grad(x, labels, out, grad_scale=out.row_loss[:1]))
+    refused(lambda: gm.sar_loss_grad(out.dlogits, labels, out, grad_scale=out.dlogits[3, 99:]))
+    refused(lambda: gm.preference_loss(x, labels, start, out, ref_logp=out.seq_logp))
+    refused(lambda: gm.preference_loss(x, labels, start, out, ref_logp=out.row_logp))
+    refused(lambda: gm.preference_loss(x, labels, start, out, grad_scale=out.pair_loss[1:]))
+    for a, b in itertools.permutations(("loss", "n_terms", "row_logp", "row_loss", "work"), 2):
+        io = gm._loss_io(x, labels, out, None, True)
+        was = getattr(io, a)
+        setattr(io, a, getattr(io, b))
+        assert gm.lib.space_sar_loss_grad(gm.ctx, C.byref(io), None) == binding.SPACE_EINVAL, (a, b)
+        setattr(io, a, was)
+    for name in ("loss", "row_logp", "row_loss", "work"):  # an output on the logits, and on the gradient
+        for place in (x, out.dlogits):
+            io = gm._loss_io(x, labels, out, None, True)
+            was = getattr(io, name)
+            setattr(io, name, place[rows - 1, V - 4:].data_ptr())
+            assert gm.lib.space_sar_loss_grad(gm.ctx, C.byref(io), None) == binding.SPACE_EINVAL, name
+            setattr(io, name, was)
+    assert "overlaps" in gm.lib.space_last_error(gm.ctx).decode()
+    # the same with copies, or between the rows of a wider buffer, is what it was
+    gm.policy_loss(x, labels, adv, out, old_logp=old - 1.0, ref_logp=ref, kl_coef=0.1)
+    want = [t.clone() for t in (out.loss, out.row_loss, out.row_kl, out.dlogits)]
+    assert int(out.n_clipped) == 2 and bool((out.row_kl > 0).all())
+    wide = torch.zeros(rows, V + 8, device="cuda")
+    wide[0, V:V + 4] = old - 1.0
+    between = tc.fresh_out(gm, rows, dlogits=wide[:, :V], pairs=2)
+    gm.policy_loss(x, labels, adv, between, old_logp=wide[0, V:V + 4], ref_logp=ref, kl_coef=0.1)
+    assert all(torch.equal(a, b) for a, b in zip(want, (between.loss, between.row_loss, between.row_kl, between.dlogits)))
+    gm.preference_loss(x, labels, start, out, ref_logp=out.seq_logp.clone())
+    torch.cuda.synchronize()
+    assert gm.device_faults() == 0

@@ -107,3 +107,33 @@ def test_dense_tensors_are_told_from_others():
         assert not binding._dense(bad), bad.shape
     assert binding._same_order(t, torch.ones(4, 6)) and not binding._same_order(t, torch.ones(6, 4).t())
     assert binding._row_stride(t[:, :3]) == 6 and binding._row_stride(t[:1, :3]) >= 3 and binding._row_stride(None) == 0
+
+
+def test_rows_that_meet_a_range_against_a_count_of_bytes(tmp_path):
+    src = tmp_path / "meet.cpp"
+    src.write_text('''#include "space_train_plan.h"
+extern "C" int meet(uint64_t x, int64_t xs, int64_t rows, int64_t cols, int64_t bytes, uint64_t lo, uint64_t hi) {
+    return space::rows_meet(x, xs, rows, cols, bytes, lo, hi);
+}
+''')
+    so = tmp_path / "meet.so"
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-Wall", "-Werror", "-I", CSRC, str(src), "-o", str(so)], check=True)
+    lib = ctypes.CDLL(str(so))
+    lib.meet.argtypes = [ctypes.c_uint64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_uint64, ctypes.c_uint64]
+    rng = random.Random(2)
+    seen = [0, 0]
+    for _ in range(5000):
+        rows, cols, b = rng.randint(1, 5), rng.randint(1, 9), rng.choice([2, 4])
+        xs = cols + rng.choice([0, rng.randint(0, 12)])
+        x, lo = 500, 500 + rng.randint(-40, rows * xs * b + 20)
+        hi = lo + rng.randint(1, 24)
+        held = {x + (r * xs + c) * b + i for r in range(rows) for c in range(cols) for i in range(b)}
+        want = not held.isdisjoint(range(lo, hi))
+        assert lib.meet(x, xs, rows, cols, b, lo, hi) == want, (xs, rows, cols, b, lo, hi)
+        seen[want] += 1
+    assert min(seen) > 500
+    # the last row of a large buffer, and the gap in front of it
+    x, xs, rows, cols = 1 << 44, (1 << 26) + 3, 4000000, 1001
+    last = x + (rows - 1) * xs * 2
+    assert lib.meet(x, xs, rows, cols, 2, last + 2 * cols - 1, last + 2 * cols + 9) and not lib.meet(x, xs, rows, cols, 2, last + 2 * cols, last + 2 * cols + 9)
+    assert lib.meet(x, xs, rows, cols, 2, last - 1, last + 1) and not lib.meet(x, xs, rows, cols, 2, last - 9, last)
