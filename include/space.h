@@ -444,7 +444,7 @@ int space_grad_norm(space_ctx *ctx, const space_grad_tensor *tensors, int32_t n_
 /* out = grad * max_norm / *norm where *norm is above max_norm and finite, else out = grad (a norm that is not finite
  * leaves the gradients as they are: the caller finds it in *norm and skips the step).
  *   norm  DEVICE float32 [1], of space_grad_norm or of the caller (several processes that added up their squares)
- * Errors: as space_grad_norm; max_norm negative or NaN; an `out` that overlaps anything but its own equal grad. */
+ * Errors: as space_grad_norm; max_norm negative or NaN; an `out` that overlaps anything but its own equal grad, or the norm. */
 int space_grad_clip(space_ctx *ctx, const space_grad_tensor *tensors, int32_t n_tensors, const float *norm, float max_norm, void *stream);
 
 /* Tuning hook (not part of the method).  space_init reads the environment variable SPACE_TUNE once, a

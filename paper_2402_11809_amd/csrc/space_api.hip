@@ -634,14 +634,16 @@ int loss_launch(space_ctx* ctx, const char* who, const space_loss_io* io, bool r
 }
 
 // Checks a list of gradients and copies it.  writes: `out` is written, so no range that is written may meet another one (but
-// for a gradient that is clipped in place): their order would decide the result.
-int grad_list(space_ctx* ctx, const char* who, const space_grad_tensor* t, int32_t n, bool writes, std::unique_ptr<GradTensor[]>* list) {
+// for a gradient that is clipped in place), or the norm, which every workgroup reads: their order would decide the result.
+int grad_list(space_ctx* ctx, const char* who, const space_grad_tensor* t, int32_t n, bool writes, const float* norm,
+              std::unique_ptr<GradTensor[]>* list) {
     if (n < 0 || (n > 0 && !t)) return fail(ctx, SPACE_EINVAL, "%s: null or negative list", who);
     std::unique_ptr<ByteRange[]> ranges;
     list->reset(new (std::nothrow) GradTensor[n > 0 ? n : 1]);
     if (writes) ranges.reset(new (std::nothrow) ByteRange[2 * (size_t)n + 1]);
     if (!*list || (writes && !ranges)) return fail(ctx, SPACE_ENOMEM, "%s: no host memory for a list of %d", who, n);
     size_t m = 0;
+    if (writes) ranges[m++] = ByteRange{(uintptr_t)norm, (uintptr_t)norm + sizeof(float), false};
     for (int32_t i = 0; i < n; ++i) {
         const size_t gb = dtype_bytes(t[i].dtype), ob = dtype_bytes(t[i].out_dtype);
         if (!gb || (writes && !ob)) return fail(ctx, SPACE_EINVAL, "%s: tensor %d: unknown dtype", who, i);
@@ -656,7 +658,7 @@ int grad_list(space_ctx* ctx, const char* who, const space_grad_tensor* t, int32
         ranges[m++] = ByteRange{o, o + (uintptr_t)t[i].n * ob, true};
     }
     if (writes && !written_apart(ranges.get(), m))
-        return fail(ctx, SPACE_EINVAL, "%s: an output overlaps another tensor of the list", who);
+        return fail(ctx, SPACE_EINVAL, "%s: an output overlaps another tensor of the list or the norm", who);
     return SPACE_OK;
 }
 
@@ -1307,7 +1309,7 @@ int space_grad_norm(space_ctx* ctx, const space_grad_tensor* tensors, int32_t n_
     if (!norm || !work || (uintptr_t)work % 8 || (uintptr_t)norm % 4)
         return fail(ctx, SPACE_EINVAL, "space_grad_norm: null argument, or norm or work not on a whole element");
     std::unique_ptr<GradTensor[]> list;
-    if (int rc = grad_list(ctx, "space_grad_norm", tensors, n_tensors, false, &list)) return rc;
+    if (int rc = grad_list(ctx, "space_grad_norm", tensors, n_tensors, false, norm, &list)) return rc;
     HIP_TRY(ctx, launch_grad_norm(list.get(), n_tensors, norm, work, (hipStream_t)stream));
     return SPACE_OK;
 }
@@ -1317,7 +1319,7 @@ int space_grad_clip(space_ctx* ctx, const space_grad_tensor* tensors, int32_t n_
     if (!norm || (uintptr_t)norm % 4) return fail(ctx, SPACE_EINVAL, "space_grad_clip: null argument, or norm not on a whole element");
     if (!(max_norm >= 0.f)) return fail(ctx, SPACE_EINVAL, "space_grad_clip: max_norm %g negative or not a number", (double)max_norm);
     std::unique_ptr<GradTensor[]> list;
-    if (int rc = grad_list(ctx, "space_grad_clip", tensors, n_tensors, true, &list)) return rc;
+    if (int rc = grad_list(ctx, "space_grad_clip", tensors, n_tensors, true, norm, &list)) return rc;
     HIP_TRY(ctx, launch_grad_clip(list.get(), n_tensors, norm, max_norm, (hipStream_t)stream));
     return SPACE_OK;
 }

@@ -961,3 +961,23 @@ def test_outputs_of_a_loss_on_its_inputs_or_on_each_other_are_refused():
     gm.preference_loss(x, labels, start, out, ref_logp=out.seq_logp.clone())
     torch.cuda.synchronize()
     assert gm.device_faults() == 0
+
+
+def test_a_norm_inside_a_clipped_gradient_is_refused():
+    """Every workgroup reads the norm: an output over it would change the scale of what is clipped later.  Beside an output it may stand, and
+    within a gradient that is only read."""
+    torch = gc.require_gpu()
+    from paper_2402_11809_amd import binding
+    gm = tc.head_model(40)
+    flat = torch.full((20001,), 2.0, device="cuda")  # a norm, then the gradients
+    flat[0] = 8.0
+    dst = torch.full((20001,), 3.0, device="cuda")
+    for norm, grads, outs in ((flat[5:6], [flat[1:]], None), (flat[20000:], [flat[1:9000], flat[9000:]], None), (dst[7:8], [flat[1:]], [dst[1:]])):
+        with pytest.raises(binding.SpaceError):
+            gm.grad_clip(binding.GradSet(gm, grads, outs), 1.0, norm=norm)
+    torch.cuda.synchronize()
+    assert bool((flat[1:] == 2.0).all()) and bool((dst == 3.0).all())
+    gm.grad_clip(binding.GradSet(gm, [flat], [dst]), 4.0, norm=flat[:1])
+    assert float(dst[0]) == 4.0 and bool((dst[1:] == 1.0).all()) and float(flat[0]) == 8.0
+    gm.grad_clip(binding.GradSet(gm, [flat[1:]]), 2.0, norm=flat[:1])
+    assert bool((flat[1:] == 0.5).all()) and float(flat[0]) == 8.0
