@@ -438,13 +438,14 @@ typedef struct space_grad_tensor {
  *   norm  DEVICE float32 [1]
  *   work  DEVICE float64 [SPACE_GRAD_WORK], the caller's: the first 16 bytes (an arrival count) are cleared once, before the first
  *         call, and left as they were by every call; the rest is scratch.  Calls that share it must be ordered
- * Errors: SPACE_EINVAL (null, negative length, unknown dtype, pointer that is not on a whole element). */
+ * Errors: SPACE_EINVAL (null, negative length, unknown dtype, pointer that is not on a whole element, norm or work overlapping
+ * a gradient or the other). */
 int space_grad_norm(space_ctx *ctx, const space_grad_tensor *tensors, int32_t n_tensors, float *norm, double *work, void *stream);
 
 /* out = grad * max_norm / *norm where *norm is above max_norm and finite, else out = grad (a norm that is not finite
  * leaves the gradients as they are: the caller finds it in *norm and skips the step).
  *   norm  DEVICE float32 [1], of space_grad_norm or of the caller (several processes that added up their squares)
- * Errors: as space_grad_norm; max_norm negative or NaN; an `out` that overlaps anything but its own equal grad, or the norm. */
+ * Errors: as of the list in space_grad_norm; max_norm negative or NaN; an `out` that overlaps anything but its own equal grad, or the norm. */
 int space_grad_clip(space_ctx *ctx, const space_grad_tensor *tensors, int32_t n_tensors, const float *norm, float max_norm, void *stream);
 
 /* Tuning hook (not part of the method).  space_init reads the environment variable SPACE_TUNE once, a

@@ -1310,6 +1310,13 @@ int space_grad_norm(space_ctx* ctx, const space_grad_tensor* tensors, int32_t n_
         return fail(ctx, SPACE_EINVAL, "space_grad_norm: null argument, or norm or work not on a whole element");
     std::unique_ptr<GradTensor[]> list;
     if (int rc = grad_list(ctx, "space_grad_norm", tensors, n_tensors, false, norm, &list)) return rc;
+    const uintptr_t at_norm = (uintptr_t)norm, at_work = (uintptr_t)work;
+    bool apart = !ranges_meet(at_norm, sizeof(float), at_work, SPACE_GRAD_WORK * sizeof(double));
+    for (int32_t i = 0; i < n_tensors && apart; ++i) {
+        const uintptr_t at = (uintptr_t)list[i].grad, bytes = (uintptr_t)list[i].n * dtype_bytes(list[i].dtype);
+        apart = !ranges_meet(at, bytes, at_norm, sizeof(float)) && !ranges_meet(at, bytes, at_work, SPACE_GRAD_WORK * sizeof(double));
+    }
+    if (!apart) return fail(ctx, SPACE_EINVAL, "space_grad_norm: norm or work overlaps a gradient or the other");
     HIP_TRY(ctx, launch_grad_norm(list.get(), n_tensors, norm, work, (hipStream_t)stream));
     return SPACE_OK;
 }

@@ -24,6 +24,11 @@ inline bool rows_meet(uintptr_t x, int64_t xs, int64_t rows, int64_t cols, size_
     return r < (uintptr_t)rows && x + r * step < hi;
 }
 
+// Whether a and b, of so many bytes, have one in common (an empty range has none).
+inline bool ranges_meet(uintptr_t a, uintptr_t a_bytes, uintptr_t b, uintptr_t b_bytes) {
+    return a_bytes && b_bytes && (a < b ? b - a < a_bytes : a - b < b_bytes);
+}
+
 struct ByteRange {
     uintptr_t lo, hi;
     bool written;

@@ -981,3 +981,27 @@ def test_a_norm_inside_a_clipped_gradient_is_refused():
     assert float(dst[0]) == 4.0 and bool((dst[1:] == 1.0).all()) and float(flat[0]) == 8.0
     gm.grad_clip(binding.GradSet(gm, [flat[1:]]), 2.0, norm=flat[:1])
     assert bool((flat[1:] == 0.5).all()) and float(flat[0]) == 8.0
+
+
+def test_a_norm_or_scratch_on_a_gradient_or_on_each_other_is_refused():
+    """The norm inside the scratch would stay in the arrival count, the scratch inside a gradient would be read as one."""
+    torch = gc.require_gpu()
+    from paper_2402_11809_amd import binding
+    gm = tc.head_model(40)
+    W = binding.SPACE_GRAD_WORK
+    buf = torch.zeros(3 * W, dtype=torch.float64, device="cuda")  # [gradient | scratch | norm]
+    g, work, norm = buf.data_ptr(), buf[W:].data_ptr(), buf[2 * W:].data_ptr()
+    buf[:W].view(torch.float32).fill_(0.5)
+    one = lambda n, dtype=0: (binding.SpaceGradTensor * 2)(binding.SpaceGradTensor(g, None, n, dtype, 0), binding.SpaceGradTensor(work, None, 0, 0, 0))
+    rc = lambda t, norm, work: gm.lib.space_grad_norm(gm.ctx, t, 2, norm, work, binding._stream())
+    for t, a, b in ((one(2 * W), work, work), (one(2 * W), work + 8 * W - 4, work), (one(2 * W), g + 8, work), (one(2 * W + 1), norm, work),
+                    (one(2 * W), norm, g + 8 * W - 8), (one(4 * W + 1, 1), norm, work), (one(4 * W + 1), work + 8 * W, work)):
+        assert rc(t, a, b) == binding.SPACE_EINVAL
+    torch.cuda.synchronize()
+    assert bool((buf[:W].view(torch.float32) == 0.5).all()) and bool((buf[W:] == 0).all())
+    for _ in range(2):
+        assert rc(one(2 * W), norm, work) == 0
+        torch.cuda.synchronize()
+        want = 0.5 * (2 * W) ** 0.5
+        assert abs(float(buf[2 * W:].view(torch.float32)[0]) - want) <= want * U * 1.001 and bool((buf[W:W + 2] == 0).all())
+        assert bool((buf[:W].view(torch.float32) == 0.5).all())

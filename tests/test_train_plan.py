@@ -137,3 +137,19 @@ extern "C" int meet(uint64_t x, int64_t xs, int64_t rows, int64_t cols, int64_t 
     last = x + (rows - 1) * xs * 2
     assert lib.meet(x, xs, rows, cols, 2, last + 2 * cols - 1, last + 2 * cols + 9) and not lib.meet(x, xs, rows, cols, 2, last + 2 * cols, last + 2 * cols + 9)
     assert lib.meet(x, xs, rows, cols, 2, last - 1, last + 1) and not lib.meet(x, xs, rows, cols, 2, last - 9, last)
+
+
+def test_ranges_that_meet_against_a_count_of_bytes(tmp_path):
+    src = tmp_path / "pair.cpp"
+    src.write_text('''#include "space_train_plan.h"
+extern "C" int meet(uint64_t a, uint64_t an, uint64_t b, uint64_t bn) { return space::ranges_meet(a, an, b, bn); }
+''')
+    so = tmp_path / "pair.so"
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-Wall", "-Werror", "-I", CSRC, str(src), "-o", str(so)], check=True)
+    lib = ctypes.CDLL(str(so))
+    lib.meet.argtypes = [ctypes.c_uint64] * 4
+    for a in range(6):
+        for an in range(5):
+            for b in range(6):
+                for bn in range(5):
+                    assert lib.meet(a, an, b, bn) == (not set(range(a, a + an)).isdisjoint(range(b, b + bn))), (a, an, b, bn)
