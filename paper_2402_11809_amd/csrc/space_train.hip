@@ -302,7 +302,8 @@ template <int KIND>
 __device__ __forceinline__ RowSlope row_slope(const PolicyArgs& p, int row, double logp) {
     RowSlope s{-logp, -1.0, 0.0, false};
     if (KIND == LOSS_POLICY) {
-        const double a = p.advantages[row], q = p.old_logp ? exp(logp - p.old_logp[row]) : 1.0;
+        // (without old_logp the ratio is logp's to itself: 1, also of a masked token, but no number where logp is none)
+        const double a = p.advantages[row], q = p.old_logp ? exp(logp - p.old_logp[row]) : isnan(logp) ? logp : 1.0;
         const double u = q * a, c = fmin(fmax(q, (double)p.lo), (double)p.hi) * a;
         s.clipped = u > c;
         s.term = s.clipped ? -c : -u;

@@ -1005,3 +1005,37 @@ def test_a_norm_or_scratch_on_a_gradient_or_on_each_other_is_refused():
         want = 0.5 * (2 * W) ** 0.5
         assert abs(float(buf[2 * W:].view(torch.float32)[0]) - want) <= want * U * 1.001 and bool((buf[W:W + 2] == 0).all())
         assert bool((buf[:W].view(torch.float32) == 0.5).all())
+
+
+# ------------------------------------------------------------------------------- what is no number, and what counts nothing
+
+@pytest.mark.parametrize("V,rows", [(40, 7), (1000, 300), (32000, 7), (40001, 210), (131079, 7)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_are_no_number_make_all_their_terms_and_gradient_nan(V, rows, dtype):
+    """Nothing but -inf, a NaN, a +inf, at the label or beside it: term, KL term, log probability and the whole gradient of the row, in the policy loss
+    also where the ratio is 1 by definition and where advantage or weight is 0.  Other rows are what they are without these."""
+    torch = gc.require_gpu()
+    gm = tc.head_model(V)
+    x, _ = tc.make_logits(np.random.default_rng(V), rows, V, dtype, lift=False)
+    labels = torch.full((rows,), V // 2, dtype=torch.int32, device="cuda")
+    clean = x.clone()
+    x[0, :] = float("-inf"); x[1, 1] = float("nan"); x[2, V - 1] = float("inf"); x[3, V // 2] = float("nan"); x[4, V // 2] = float("inf")
+    bad = torch.arange(rows, device="cuda") < 5
+    ones = torch.ones(rows, device="cuda")
+    zeros = torch.zeros(rows, device="cuda")
+    for call, names in ((lambda a, o: gm.sar_loss_grad(a, labels, o), ("row_loss", "row_logp")),
+                        (lambda a, o: gm.policy_loss(a, labels, ones, o), ("row_loss", "row_logp")),
+                        (lambda a, o: gm.policy_loss(a, labels, -ones, o, old_logp=-ones, ref_logp=-ones, kl_coef=0.1, mean=False), ("row_loss", "row_logp", "row_kl")),
+                        (lambda a, o: gm.policy_loss(a, labels, zeros, o, row_weight=zeros), ("row_loss", "row_logp"))):
+        out, ref = tc.fresh_out(gm, rows, dtype), tc.fresh_out(gm, rows, dtype)
+        call(x, out), call(clean, ref)
+        torch.cuda.synchronize()
+        for n in names:
+            assert bool(torch.isnan(getattr(out, n)[bad]).all()), n
+            assert torch.equal(getattr(out, n)[~bad], getattr(ref, n)[~bad]), n
+        assert bool(torch.isnan(out.dlogits[bad]).all()) and torch.equal(out.dlogits[~bad], ref.dlogits[~bad])
+        assert np.isnan(float(out.loss)) and int(out.n_terms) == rows
+        bare = tc.fresh_out(gm, rows)
+        call(x, bare)
+        torch.cuda.synchronize()
+        assert bool(torch.isnan(bare.row_loss[bad]).all()) and np.isnan(float(bare.loss))
