@@ -387,7 +387,9 @@ int space_sar_loss_grad(space_ctx *ctx, const space_loss_io *io, void *stream);
 /* Clipped policy loss with a KL term, for rollouts of this model (labels = the tokens that were generated):
  *   q = exp(logp - old_logp), u = q * advantage, c = clamp(q, 1 - clip_low, 1 + clip_high) * advantage,
  *   term = row_weight * (-min(u, c) + kl_coef * (exp(d) - d - 1)),  d = ref_logp - logp.
- * The gradient of a row whose u is above its c (clipped) is that of the KL term alone; at u == c it is u's. */
+ * The gradient of a row whose u is above its c (clipped) is that of the KL term alone; at u == c it is u's.  An advantage or a
+ * weight of 0 makes its product 0 also where the other factor is infinite (a log probability of -inf or of the type's lowest value;
+ * not where it is NaN).  Where the slope along logp is infinite and counts, the row's gradient is infinite or NaN. */
 typedef struct space_policy_params {
     const float *advantages; /* [rows] */
     const float *old_logp;   /* [rows] logp under the model that generated the tokens; NULL: logp itself, held constant (q = 1) */

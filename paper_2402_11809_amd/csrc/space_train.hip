@@ -294,6 +294,9 @@ __device__ __forceinline__ int sum_of(const int* s) {
     return n;
 }
 
+// v * by, and 0 where `by` is 0 though v is infinite: nothing is contributed, as for every finite v (NaN stays NaN).
+__device__ __forceinline__ double times(double v, double by) { return by == 0.0 && isinf(v) ? 0.0 : v * by; }
+
 struct RowSlope {
     double term, slope, kl;
     bool clipped;
@@ -304,7 +307,7 @@ __device__ __forceinline__ RowSlope row_slope(const PolicyArgs& p, int row, doub
     if (KIND == LOSS_POLICY) {
         // (without old_logp the ratio is logp's to itself: 1, also of a masked token, but no number where logp is none)
         const double a = p.advantages[row], q = p.old_logp ? exp(logp - p.old_logp[row]) : isnan(logp) ? logp : 1.0;
-        const double u = q * a, c = fmin(fmax(q, (double)p.lo), (double)p.hi) * a;
+        const double u = times(q, a), c = fmin(fmax(q, (double)p.lo), (double)p.hi) * a;
         s.clipped = u > c;
         s.term = s.clipped ? -c : -u;
         s.slope = s.clipped ? 0.0 : -u;
@@ -317,8 +320,9 @@ __device__ __forceinline__ RowSlope row_slope(const PolicyArgs& p, int row, doub
             }
         }
         if (p.row_weight) {
-            s.term *= p.row_weight[row];
-            s.slope *= p.row_weight[row];
+            const double w = p.row_weight[row];
+            s.term = times(s.term, w);
+            s.slope = times(s.slope, w);
         }
     }
     return s;

@@ -1039,3 +1039,48 @@ def test_rows_that_are_no_number_make_all_their_terms_and_gradient_nan(V, rows, 
         call(x, bare)
         torch.cuda.synchronize()
         assert bool(torch.isnan(bare.row_loss[bad]).all()) and np.isnan(float(bare.loss))
+
+
+@pytest.mark.parametrize("rows", [12, 300])  # added up by the rows, and by a launch behind them
+def test_an_advantage_or_weight_of_zero_takes_infinite_factors_away(rows):
+    """Ratios that are infinite (a token that the old model gave no chance, as -inf or as the lowest number) with an advantage of 0, KL terms that are
+    infinite (masked now, or by the reference) with a weight of 0: nothing is contributed, as for every finite factor."""
+    torch = gc.require_gpu()
+    V, inf, low = 64, float("inf"), torch.finfo(torch.float32).min
+    gm = tc.head_model(V)
+    x, _ = tc.make_logits(np.random.default_rng(4), rows, V, "f32")
+    labels = torch.full((rows,), 9, dtype=torch.int32, device="cuda")
+    f = lambda *v: torch.tensor(list(v) + [1.0] * (rows - len(v)), device="cuda")
+    x[4, 9] = -inf
+    #      0     1    2     3     4     5     6
+    adv = f(0.0, 0.0, -0.0, 1.0, 1.0, -1.0, 0.0)
+    wgt = f(1.0, 1.0, 1.0, 0.0, 0.0, 0.0, 1.0)
+    old = f(-inf, low, -800.0, -2.0, -2.0, -inf, -inf)
+    ref = f(-2.0, -2.0, -2.0, -inf, -2.0, -2.0, -2.0)
+    old[7:], ref[7:] = -2.0, -2.0
+    out = tc.fresh_out(gm, rows, "f32")
+    gm.policy_loss(x, labels, adv, out, old_logp=old, ref_logp=ref, row_weight=wgt, mean=False)
+    torch.cuda.synchronize()
+    assert bool((out.row_loss[:7] == 0).all()) and bool((out.dlogits[:7] == 0).all())
+    lp = tc.Rows64(x[7:], labels[7:]).logp
+    q = torch.exp(lp + 2.0)
+    rest = -torch.minimum(q, q.clamp(max=float(np.float32(1) + np.float32(0.2))))
+    t = 300 * U  # logp of some 10, its sum of 64 terms, the exponential: less than that, relative
+    assert bool(((out.row_loss[7:].double() - rest).abs() <= t * rest.abs()).all()) and abs(float(out.loss) - float(rest.sum())) <= t * float(rest.abs().sum())
+    assert int(out.n_clipped) == int((q > 1.2).sum())
+    # with a KL term: its part alone where the advantage is 0, nothing where the weight is
+    gm.policy_loss(x, labels, adv, out, old_logp=old, ref_logp=ref, row_weight=wgt, kl_coef=0.5, mean=False)
+    torch.cuda.synchronize()
+    lp = tc.Rows64(x, labels).logp
+    assert bool((out.row_loss[3:6] == 0).all()) and bool((out.dlogits[3:6] == 0).all())
+    for r in (0, 1, 2, 6):
+        gap = -2.0 - lp[r]
+        want = 0.5 * float(torch.expm1(gap) - gap)
+        assert abs(float(out.row_loss[r]) - want) <= 300 * U * (abs(want) + float(gap.abs())), r
+        p = torch.softmax(x[r].double(), 0)
+        p[9] -= 1.0
+        c = 0.5 * float(torch.expm1(gap))
+        assert bool(((out.dlogits[r].double() - c * p).abs() <= 300 * U * (abs(c) + 1) * (p.abs() + U)).all()), r
+    # an infinite factor that does count stays infinite
+    gm.policy_loss(x, labels, -torch.ones(rows, device="cuda"), out, old_logp=old, mean=False)
+    assert bool((out.row_loss[[0, 1, 2, 5, 6]] == inf).all()) and float(out.loss) == inf
