@@ -1084,3 +1084,125 @@ def test_an_advantage_or_weight_of_zero_takes_infinite_factors_away(rows):
     # an infinite factor that does count stays infinite
     gm.policy_loss(x, labels, -torch.ones(rows, device="cuda"), out, old_logp=old, mean=False)
     assert bool((out.row_loss[[0, 1, 2, 5, 6]] == inf).all()) and float(out.loss) == inf
+
+
+# ------------------------------------------------------------------------------- calls that count and add up in launches of their own
+
+# rows above what a call adds up by itself, for every width of the rows' kernels in both types; and on both sides of that border
+LARGE = [(1000, 700, "f32"), (2048, 193, "bf16"), (2049, 193, "f32"), (4096, 260, "bf16"), (4099, 300, "f32"), (8192, 260, "f32"), (8200, 300, "f32"), (8200, 300, "bf16"),
+         (20000, 1600, "f32"), (20000, 500, "bf16"), (32771, 4097, "f32"), (32771, 4097, "bf16"), (65543, 4097, "f32"), (65543, 4097, "bf16"), (131079, 4097, "bf16"),
+         (1000, 192, "f32"), (1000, 193, "f32"), (32000, 976, "bf16"), (32000, 977, "bf16"), (32000, 3906, "f32"), (32000, 3907, "f32")]
+
+
+def _rows_on_gpu(V, rows, dtype):
+    """As tc.make_logits, drawn on the GPU: N(0, 2), labels lifted, a fifth left out."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(V + rows)
+    x = torch.randn((rows, V), generator=g, device="cuda").mul_(2.0)
+    labels = torch.randint(0, V, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    x.scatter_add_(1, labels.long()[:, None], torch.rand((rows, 1), generator=g, device="cuda") * 14.0)
+    labels[torch.rand(rows, generator=g, device="cuda") < 0.2] = -1
+    return x.to(tc.torch_type(dtype)), labels, lambda std: torch.randn(rows, generator=g, device="cuda") * std
+
+
+@pytest.mark.parametrize("V,rows,dtype", LARGE)
+def test_losses_of_many_rows_against_the_formulas(V, rows, dtype):
+    """The finetuning and the policy loss, mean, scaled: terms, counts, loss and gradient, with every row's tolerance as in the tests of few rows."""
+    torch = gc.require_gpu()
+    gm = tc.head_model(V)
+    x, labels, noise = _rows_on_gpu(V, rows, dtype)
+    ref = tc.Rows64(x, labels)
+    n = int(ref.keep.sum())
+    assert 0 < n < rows
+    scale = torch.tensor([0.5], device="cuda")
+    out = tc.fresh_out(gm, rows, dtype)
+    gm.sar_loss_grad(x, labels, out, mean=True, grad_scale=scale)
+    torch.cuda.synchronize()
+    ref.check_logp(out.row_logp)
+    ref.check_logp(out.row_loss, -1.0)
+    assert int(out.n_terms) == n
+    total = float(ref.logp.sum())
+    assert abs(float(out.loss) + total / n) <= _loss_tol(ref.logp, ref.logp_tol) / n + abs(total) / n * U
+    c = torch.full_like(ref.logp, 0.5 / n)
+    ref.check_gradient(out.dlogits, -c, c * 2 * U, dtype)
+    del out
+    adv, old, refp, weight = noise(1.0), ref.logp.float() + noise(0.4), ref.logp.float() + noise(0.5), noise(1.0).abs()
+    out = tc.fresh_out(gm, rows, dtype)
+    gm.policy_loss(x, labels, adv, out, old_logp=old, ref_logp=refp, clip_low=0.2, clip_high=0.3, kl_coef=0.3, row_weight=weight, mean=True, grad_scale=scale)
+    torch.cuda.synchronize()
+    ref.check_logp(out.row_logp)
+    A, w, k = adv.double(), weight.double(), float(np.float32(0.3))
+    q = torch.exp(ref.logp - old.double())
+    lo, hi = float(np.float32(1) - np.float32(0.2)), float(np.float32(1) + np.float32(0.3))
+    u, cl = q * A, q.clamp(lo, hi) * A
+    t = ref.logp_tol + 4 * U
+    gap = refp.double() - ref.logp
+    # a ratio that is as near a border of the clamp as its own error goes either way: its row is left to the bound of both sides
+    edge = ref.keep & (((q - lo).abs() <= q * t) | ((q - hi).abs() <= q * t))
+    clipped = ref.keep & (u > cl)
+    zero = torch.zeros_like(u)
+    term = torch.where(ref.keep, w * (-torch.minimum(u, cl) + k * (torch.expm1(gap) - gap)), zero)
+    term_tol = torch.where(ref.keep, w * (u.abs() + k * (torch.expm1(gap).abs() + 1) * (1 + t)) * t + term.abs() * U, zero)
+    assert bool(((out.row_loss.double() - term).abs() <= term_tol).all())
+    kl = torch.where(ref.keep, torch.expm1(gap) - gap, zero)
+    assert bool(((out.row_kl.double() - kl).abs() <= torch.expm1(gap).abs() * t + kl.abs() * 2 * U + t * t).all())
+    assert int(out.n_terms) == n and abs(int(out.n_clipped) - int(clipped.sum())) <= int(edge.sum()) and 0 < int(out.n_clipped) < n
+    assert abs(float(out.loss) - float(term.sum()) / n) <= _loss_tol(term, term_tol) / n
+    slope = -w * (torch.where(clipped, zero, u) + k * torch.expm1(gap))
+    slope_tol = w * (u.abs() + k * torch.exp(gap)) * (t + 2 * U) + torch.where(edge, w * u.abs(), zero)
+    ref.check_gradient(out.dlogits, slope * (0.5 / n), (slope_tol + slope.abs() * 3 * U) * (0.5 / n), dtype)
+    assert gm.device_faults() == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,fill", [(40, 0), (1000, 0), (1000, 130), (5003, 130), (32000, 0), (32000, 130), (131079, 0), (131079, 130)])
+def test_preference_loss_of_masked_and_infinite_logits(V, fill, dtype):
+    """Masks as in the finetuning loss: -inf and the type's lowest value beside the label, the label alone, a masked label in the chosen and in the
+    rejected sequence, a NaN in one pair, anything in rows that do not count; in one launch behind the rows and in three (fill)."""
+    torch = gc.require_gpu()
+    gm = tc.head_model(V)
+    t, inf = tc.torch_type(dtype), float("inf")
+    start = [0, 3, 6, 8, 10, 12, 14, 16, 19, 19 + fill, 19 + 2 * fill]
+    rows, y = start[-1], V // 2
+    x, _ = tc.make_logits(np.random.default_rng(V), rows, V, dtype, lift=False)
+    labels = torch.full((rows,), y, dtype=torch.int32, device="cuda")
+    low = torch.finfo(t).min
+    x[0, :y] = -inf                                       # pair 0: masks beside the label
+    x[1, y + 1:] = -inf
+    x[2, :] = -inf; x[2, y] = 1.5                         # the label alone
+    x[3, :] = low; x[3, y] = 0.25; x[3, V - 1] = 0.25
+    x[4, :] = low
+    x[5, ::2] = -inf; x[5, y] = 0.0
+    x[7, 1] = float("nan")                                # pair 1: a NaN
+    x[13, y] = -inf                                       # pair 2: the rejected label masked
+    x[14, y] = -inf                                       # pair 3: the chosen label masked
+    labels[16] = -1; x[16, :] = -inf                      # rows that do not count
+    labels[9] = -5; x[9, 0] = float("nan")
+    labels[11] = -1; x[11, 0] = inf
+    out = tc.fresh_out(gm, rows, dtype, pairs=5)
+    gm.preference_loss(x, labels, torch.tensor(start, dtype=torch.int32, device="cuda"), out, beta=0.25, mean=False)
+    torch.cuda.synchronize()
+    fine = [r for r in range(rows) if r not in (6, 7, 8, 9)]
+    ref = tc.Rows64(x[fine].nan_to_num(nan=0.0, posinf=0.0, neginf=-inf), labels[fine])
+    assert bool(torch.isnan(out.dlogits[[6, 7, 8]]).all()) and np.isnan(float(out.pair_loss[1])) and np.isnan(float(out.loss)) and np.isnan(float(out.row_logp[7]))
+    assert bool((out.dlogits[[9, 11, 16]] == 0).all()) and bool((out.row_logp[[9, 11, 16]] == 0).all())
+    assert float(out.pair_loss[2]) == 0.0 and float(out.pair_loss[3]) == inf and float(out.seq_logp[5]) == -inf and float(out.seq_logp[6]) == -inf
+    # slopes: those of pairs 2 and 3 are limits, 0 and -beta
+    S = [ref.logp[[fine.index(r) for r in range(a, b)]].sum() if r0 != 1 else None for r0, a, b in zip([0, 0, 1, 1, 2, 2, 3, 3, 4, 4], start[:-1], start[1:])]
+    tol = [ref.logp_tol[[fine.index(r) for r in range(a, b)]].sum() if r0 not in (1, 2, 3) else None for r0, a, b in
+           zip([0, 0, 1, 1, 2, 2, 3, 3, 4, 4], start[:-1], start[1:])]
+    c, c_tol = torch.zeros(len(fine), dtype=torch.float64, device="cuda"), torch.zeros(len(fine), dtype=torch.float64, device="cuda")
+    for p in (0, 2, 3, 4):
+        z_tol = 0.0
+        slope = {2: 0.0, 3: -0.25}.get(p)
+        if slope is None:
+            z = 0.25 * (S[2 * p] - S[2 * p + 1])
+            z_tol = 0.25 * float(tol[2 * p] + tol[2 * p + 1]) + 4 * U * float(abs(S[2 * p]) + abs(S[2 * p + 1]))
+            slope = -0.25 * float(torch.sigmoid(-z))
+            want = float(torch.nn.functional.softplus(-z, threshold=50))
+            assert abs(float(out.pair_loss[p]) - want) <= z_tol + want * 2 * U, p
+        for which, sign in ((0, 1.0), (1, -1.0)):
+            for r in range(start[2 * p + which], start[2 * p + which + 1]):
+                c[fine.index(r)], c_tol[fine.index(r)] = sign * slope, 0.25 * z_tol + abs(slope) * 4 * U
+    ref.check_gradient(out.dlogits[fine], c, c_tol, dtype)
+    assert gm.device_faults() == 0
