@@ -810,7 +810,7 @@ __device__ __forceinline__ double chunk_squares(const T* __restrict__ x, int n) 
     typedef Vec<T> V;
     constexpr int E = V::N, NV = kGradChunk / kGradThreads / E;
     double sum[2] = {0.0, 0.0};
-    const int tid = threadIdx.x, whole = n / E, odd = whole * E + tid;
+    const int tid = threadIdx.x % kGradThreads, whole = n / E, odd = whole * E + tid;
     typename V::raw q[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -832,9 +832,9 @@ __device__ __forceinline__ double chunk_squares(const T* __restrict__ x, int n) 
 
 // One chunk after another, dealt out to the workgroups; those from kept_from on stay in the cache.
 template <bool KEPT>
-__device__ __forceinline__ double list_squares(const GradList& g, int c, int end) {
+__device__ __forceinline__ double list_squares(const GradList& g, int c, int end, int step) {
     double sum = 0.0;
-    for (; c < end; c += gridDim.x) {
+    for (; c < end; c += step) {
         const int t = grad_tensor_of(g, c), n = chunk_elements(g, t, c);
         const int64_t from = (int64_t)(c - g.first[t]) * kGradChunk;
         if (g.last[t] & 0x4000) sum += chunk_squares<uint16_t, KEPT>((const uint16_t*)g.grad[t] + from, n);
@@ -849,18 +849,22 @@ __device__ __forceinline__ void sum_squares(const double* work, int parts, float
     sum = block_sum<THREADS / 64>(sum, s);
     if (threadIdx.x == 0) *norm = (float)sqrt(sum);
 }
-// arrived: a lone launch of few workgroups, the last of which takes the root; else a launch behind them does
-__global__ __launch_bounds__(kGradThreads) void grad_square_kernel(GradList g, int kept_from, double* work, int first_launch, uint32_t* arrived,
-                                                                   float* norm) {
-    __shared__ double s[kGradThreads / 64];
+// A workgroup takes CHUNKS chunks at a time, kGradThreads threads each.  LAST: a lone launch of few workgroups, the last of which takes the
+// root; else a launch behind them does.
+template <int CHUNKS, bool LAST>
+__global__ __launch_bounds__(kGradThreads * CHUNKS) void grad_square_kernel(GradList g, int kept_from, double* work, int first_launch, uint32_t* arrived,
+                                                                            float* norm) {
+    constexpr int THREADS = kGradThreads * CHUNKS;
+    __shared__ double s[THREADS / 64];
     __shared__ int s_last;
-    const int mine = blockIdx.x, step = gridDim.x;
-    double sum = list_squares<false>(g, mine, kept_from);
-    const int turns = max(kept_from - mine + step - 1, 0) / step;  // how many of those this workgroup had
-    sum += list_squares<true>(g, mine + turns * step, g.first[g.count]);
-    sum = block_sum<kGradThreads / 64>(sum, s);
+    // (the same for all threads of a wave)
+    const int mine = blockIdx.x * CHUNKS + __builtin_amdgcn_readfirstlane(threadIdx.x / kGradThreads), step = gridDim.x * CHUNKS;
+    double sum = list_squares<false>(g, mine, kept_from, step);
+    const int turns = max(kept_from - mine + step - 1, 0) / step;  // how many of those these threads had
+    sum += list_squares<true>(g, mine + turns * step, g.first[g.count], step);
+    sum = block_sum<THREADS / 64>(sum, s);
     if (threadIdx.x == 0) __hip_atomic_store(work + blockIdx.x, first_launch ? sum : work[blockIdx.x] + sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (arrived && arrive(arrived, &s_last)) sum_squares<kGradThreads, true>(work, gridDim.x, norm, s);
+    if (LAST && arrive(arrived, &s_last)) sum_squares<THREADS, true>(work, gridDim.x, norm, s);
 }
 __global__ __launch_bounds__(1024) void grad_norm_kernel(const double* work, int parts, float* norm) {
     __shared__ double s[16];
@@ -974,24 +978,29 @@ hipError_t each_grad_list(const GradTensor* t, int n, F launch) {
 
 int grad_workgroups(int chunks) { return chunks < kGradParts ? chunks : kGradParts; }
 
-// Workgroups up to which the last one takes the root itself: one launch less, but each adds to one count, 14 ns.  On the GPU alone that is
-// level at 128 (16 workgroups 5.8 us in one launch, 6.6 apart; 128 6.5 and 6.6, 256 8.0 and 6.6, 384 9.8 and 6.7), but a call of
-// this size waits for the host, which makes the launches: norm and clipping of 265 chunks 13.3 us in one, 14.4 apart.
-constexpr int kGradSmall = 288;
+// Chunks up to which the last workgroup takes the root itself: one launch less, but each workgroup adds to one count, 14 ns, so from kGradSingle
+// on a workgroup takes two chunks at a time (us of norm and clipping in replayed graphs, one / two / a launch behind: 16 chunks 8.1 / 8.3 / 9.0, 48 8.5 / 8.7 /
+// 9.2, 96 9.1 / 8.9 / 9.2, 192 10.4 / 9.7 / 9.5, 288 12.1 / 10.4 / 10.0, 384 13.3 / 12.0 / 10.1).  On the GPU alone two and a launch behind
+// cross at 170 (behind other work 128 11.3 / 11.6, 192 11.8 / 11.6, 288 12.8 / 12.4, 384 13.8 / 12.7); where the host's launches are waited for, a
+// call by itself at 320 (192 23.2 / 24.1, 288 24.1 / 24.4, 320 24.4 / 24.4, 384 25.0 / 24.4) and calls in a row later (320 12.7 / 15.3, 512 14.8 /
+// 15.3).  The border is that of a call by itself, in which both count.
+constexpr int kGradSingle = 64, kGradSmall = 320;
 
 hipError_t launch_grad_norm(const GradTensor* t, int n, float* norm, double* work, hipStream_t s) {
     uint32_t* arrived = (uint32_t*)work;
     work += 2;
     // a later launch adds to the partial sums of an earlier one, so all of them have as many workgroups
-    int parts = 0, lists = 0, first = 1;
+    int chunks = 0, lists = 0, first = 1;
     hipError_t e = each_grad_list(t, n, [&](const GradList& g, int) {
-        parts = max(parts, grad_workgroups(g.first[g.count]));
+        chunks = max(chunks, g.first[g.count]);
         ++lists;
     });
     if (e != hipSuccess) return e;
-    const bool small = lists == 1 && parts <= kGradSmall;
+    const bool small = lists == 1 && chunks <= kGradSmall;
+    const int parts = !small ? grad_workgroups(chunks) : chunks <= kGradSingle ? chunks : (chunks + 1) / 2;
     e = each_grad_list(t, n, [&](const GradList& g, int kept_from) {
-        hipLaunchKernelGGL(grad_square_kernel, dim3(parts), dim3(kGradThreads), 0, s, g, kept_from, work, first, small ? arrived : nullptr, norm);
+        const auto kernel = !small ? grad_square_kernel<1, false> : chunks <= kGradSingle ? grad_square_kernel<1, true> : grad_square_kernel<2, true>;
+        hipLaunchKernelGGL(kernel, dim3(parts), dim3(small && chunks > kGradSingle ? 2 * kGradThreads : kGradThreads), 0, s, g, kept_from, work, first, arrived, norm);
         first = 0;
     });
     if (e != hipSuccess || small) return e;

@@ -1206,3 +1206,44 @@ def test_preference_loss_of_masked_and_infinite_logits(V, fill, dtype):
                 c[fine.index(r)], c_tol[fine.index(r)] = sign * slope, 0.25 * z_tol + abs(slope) * 4 * U
     ref.check_gradient(out.dlogits[fine], c, c_tol, dtype)
     assert gm.device_faults() == 0
+
+
+@pytest.mark.parametrize("types", [["f32"], ["bf16", "f32"]])
+@pytest.mark.parametrize("chunks", [1, 2, 17, 63, 64, 65, 66, 127, 129, 200, 319, 320, 321, 1000, 2048, 2049, 4500])
+def test_norms_of_so_many_chunks(chunks, types):
+    """On both sides of what takes the root in the squares' own launch and of the workgroups of a launch: norm and clipping against 64 bits, twice
+    with one scratch, and in a graph that is replayed with other gradients; norm: one rounding of a 64-bit sum."""
+    torch = gc.require_gpu()
+    from paper_2402_11809_amd import binding
+    gm = tc.head_model(40)
+    g = torch.Generator(device="cuda").manual_seed(chunks)
+    k = min(chunks, 7)
+    sizes = [8192 * (chunks // k)] * (k - 1)
+    sizes.append(8192 * (chunks - (chunks // k) * (k - 1)) - 5)
+    grads = [torch.empty(n, dtype=tc.torch_type(types[i % len(types)]), device="cuda") for i, n in enumerate(sizes)]
+    outs = [torch.empty(n, device="cuda") for n in sizes]
+    gs = binding.GradSet(gm, grads, outs)
+
+    def check():
+        torch.cuda.synchronize()
+        want = _norm64(grads)
+        assert abs(float(gs.norm) - want) <= want * U * 1.001 and bool((gs.work[:2] == 0).all())
+        for a, o in zip(grads, outs):
+            exact = a.double() * (0.5 / want)
+            assert bool(((o.double() - exact).abs() <= exact.abs() * 4 * U).all())
+
+    def draw():
+        for a in grads:
+            a.copy_(torch.randn(a.shape, generator=g, device="cuda"))
+
+    for _ in range(2):
+        draw(), tc.spoil(gs.work[2:]), gm.grad_clip(gs, 0.5), check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gm.grad_clip(gs, 0.5)
+    for _ in range(3):
+        draw(), tc.spoil(gs.norm)
+        graph.replay()
+        check()
+        gm.grad_clip(gs, 0.5)
+        check()
