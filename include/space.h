@@ -408,6 +408,7 @@ int space_policy_loss(space_ctx *ctx, const space_loss_io *io, const space_polic
  * of s that count (average: their mean; 0 for a sequence without any).
  *   z = beta * ((S_2p - ref_2p) - (S_2p+1 - ref_2p+1)) - margin
  *   term_p = (1 - smoothing) * softplus(-z) + smoothing * softplus(z)
+ * A pair of which both S are -inf (a masked label on either side) has a z, a term and a gradient that are NaN.
  * Rows in front of the first and behind the last sequence do not count (their row_logp is written all the same).  Offsets outside
  * 0 .. rows or in falling order are clamped and counted by space_device_faults(); which rows a sequence then has is unspecified. */
 typedef struct space_preference_params {

@@ -369,7 +369,9 @@ def _row_stride(t) -> int:
 class GradSet:
     """The gradients of a model as space_grad_norm / space_grad_clip take them: `grads` CUDA tensors (float32 or bfloat16, dense in
     any order of dimensions), `outs` where the clipped ones go (same shapes and strides; None: in place).  Reusable as long as the
-    tensors stay where they are, which the set sees to by holding them; norm and scratch belong to the set."""
+    tensors stay where they are, which the set sees to by holding them; norm and scratch belong to the set.  It knows the tensors,
+    not the parameters: a loop that drops its gradients (zero_grad with set_to_none, torch's default) has new ones every step and needs
+    a new set, as this one would go on with the old ones; one that zeroes them in place keeps its set."""
 
     def __init__(self, model: "Model", grads: Sequence[object], outs: Optional[Sequence[object]] = None):
         import torch

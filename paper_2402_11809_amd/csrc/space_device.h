@@ -64,9 +64,10 @@ __device__ __forceinline__ float row_groups_sum(float v) {
 
 // e^d for d <= 0 within about an ulp: p = d log2(e) is rounded to 32 bits, which alone would put up to 1e-6 on an
 // exponential of -20 and a bias on the sums; what it lost, d - p ln 2, goes back in behind the hardware's exponential (0.9 us
-// of the 37 of the loss over 1366 rows of 32000).  d = -inf
-// (a masked logit) or below -2.3e38, where p is infinite (the lowest value of the type as a mask), gives 0: what was lost is no
-// number or infinite there, and the limits of +-1, which no other argument reaches, drop it; NaN stays NaN.
+// of the 37 of the loss over 1366 rows of 32000).  What was
+// lost is at most |d| 2^-23, so it passes the limits of +-1 only where d is below -8e6 and the exponential has long been 0; the limits keep
+// 0 times it 0 where it is infinite or no number: d = -inf (a masked logit) or below -2.3e38, where p is infinite (the lowest value of the
+// type as a mask).  NaN stays NaN, by way of the exponential.
 __device__ __forceinline__ float exp_below(float d) {
     const float p = d * 1.4426950408889634f, e = __builtin_amdgcn_exp2f(p);
     return fmaf(e, __builtin_amdgcn_fmed3f(fmaf(p, -0.6931471805599453f, d), -1.f, 1.f), e);

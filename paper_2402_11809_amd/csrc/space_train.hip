@@ -385,7 +385,11 @@ __device__ __forceinline__ void finish_rows(const LossLaunch& l, const PolicyArg
 // A row in the registers of one workgroup: read once, written once.  Bound by memory: a row that is read while another one
 // of the CU is computed or written, so what counts is that two rows or more share a CU (128 registers a thread, four waves a
 // SIMD).  32 elements a thread in short rows, 64 in longer ones.  KEEP: the exponentials take the logits' place, 32 bits each;
-// otherwise (bf16 rows that would fill the CU that way) the packed logits stay and the exponential is taken again.
+// otherwise (bf16 rows that would fill the CU that way) the packed logits stay and the exponential is taken again, without
+// exp_below's correction: it is off by |x - max| 2^-24 of itself at most, 5e-6 before it vanishes, against bf16's half step of 4e-3.
+// The 64-bit functions of the policy loss' slope do not all fit beside a full row: the bf16 kernels that keep it packed and have the sums
+// in them (up to 4096 rows) spill 36 bytes a thread, the fp32 ones of 512 and 1024 threads without them 16 and 12 (policy and finetuning
+// loss: 2000 rows of 64000 in bf16 122 and 112 us, in fp32 198 and 193; 1000 of 128000 in bf16 137 and 122; 4200 of 40001 in fp32 276 and 267).
 // 5.77 TB/s read and written in fp32 (4096 rows of 32000, 182 us), 5.46 in bf16 (8192 rows, 192 us), where a copy of such
 // buffers reaches 4.8 - 4.9; all in one launch of 1024 threads and 32 elements 5.0 and 4.0.  Loads and stores are non-temporal:
 // stores 5.1 -> 5.5 TB/s.
@@ -627,8 +631,9 @@ __global__ __launch_bounds__(1024) void pref_pairs_kernel(LossLaunch l, PrefArgs
 __global__ __launch_bounds__(1024) void pref_sum_kernel(LossLaunch l, PrefArgs p) { sum_pairs(l, p); }
 
 // The gradient of the preference loss, a row to a workgroup.  A row's coefficient is known when its whole pair has been read, so the
-// logits are read twice; the last rows first, which the memory-side cache still holds from the first time (7264 rows of 32000 in
-// bf16, six in ten counting: both passes 197 -> 171 us).
+// logits are read twice; the last rows first, which the memory-side cache still holds from the first time (6820 rows of 32000 in
+// bf16, six in ten counting: the whole call 158 us, first rows first 160; 3000 rows in fp32 127 and 128).  The row's factors are rounded to 32
+// bits before their product is: 1.5 units in the last place of a 32-bit gradient, beside the exponential's own.
 template <typename T, int THREADS>
 __device__ __forceinline__ void pref_row(const LossLaunch& l, int row, int label, float slope) {
     T* d = (T*)l.dlogits + (size_t)row * l.dlogits_stride;
