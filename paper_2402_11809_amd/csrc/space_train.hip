@@ -142,7 +142,8 @@ __device__ __forceinline__ void sum_rows(const LossLaunch& l, int32_t* n_clipped
 }
 
 // ---- the preference loss
-// Sequence `seq` by one wave: its rows (clamped to those there are), how many count, and their sum or mean of logp.
+// Sequence `seq` by one wave: its rows (clamped to those there are), how many count, and their sum or mean of logp, added in 64 bits as they are
+// given out, rounded to 32 bits each (what their own sums of exponentials are off by is more).
 struct SeqSum {
     int from, to, n;
     double sum;
